@@ -4,3 +4,4 @@ marshals arguments (torch supplies device memory and the stream)."""
 from .binding import (  # noqa: F401
     AsdError, AsdSampler, RoundStats, RunStats, lib_path, load_library, EXPORTED_SYMBOLS, ddpm_schedule,
 )
+from .operators import AsdOps, OPS_SYMBOLS, default_ops  # noqa: F401

@@ -9,7 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libasd_b200.so")
-SOURCES = ["asd_api.cu", "asd_kernels.cu", "asd_resident.cu", "asd_gemm.cu", "asd_mlp_fused.cu", "asd_static.cu", "asd_schedule.cu"]
+SOURCES = ["asd_api.cu", "asd_kernels.cu", "asd_resident.cu", "asd_gemm.cu", "asd_mlp_fused.cu", "asd_static.cu", "asd_schedule.cu",
+           "asd_ops_api.cu", "asd_ops_rows.cu", "asd_ops_gemm.cu"]
 
 
 def _newest(paths):
@@ -20,7 +21,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     srcs = [os.path.join(HERE, "csrc", s) for s in SOURCES]
     deps = srcs + [os.path.join(HERE, "csrc", "asd_internal.h"), os.path.join(HERE, "csrc", "asd_device.cuh"),
                    os.path.join(HERE, "csrc", "asd_tc.cuh"),
-                   os.path.join(ROOT, "include", "asd.h")]
+                   os.path.join(HERE, "csrc", "asd_ops_internal.h"), os.path.join(HERE, "csrc", "asd_ops_tc.cuh"),
+                   os.path.join(ROOT, "include", "asd.h"), os.path.join(ROOT, "include", "asd_ops.h")]
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(deps):
         return LIB
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"

@@ -1,0 +1,538 @@
+// The matrix products of the gated MLP and of the 8-bit projection on the 5th-generation tensor cores:
+//   C[m, n] = sum_k A(m, k) B(n, k)
+// with either operand read along k (a row-major matrix [m or n, k]) or across it (the transpose of a row-major [k, m or n]),
+// so that the three products of a gradient need no transposed copy.
+//
+// op_pair_kernel: a cluster of two CTAs computes a 256 x BN tile with tcgen05.mma.cta_group::2.  In each CTA one thread
+// loads its own 128 rows of A and BN / 2 rows of B by TMA, one thread of the first CTA issues the MMAs, and eight warps
+// take the CTA's 128 x BN accumulator out of tensor memory, which is double-buffered: a tile's epilogue runs under the next
+// tile's MMAs.  Clusters are persistent and walk over the tiles in bands of eight tile rows, so that the tiles that are in
+// flight together share their operands in L2.
+//
+// Epilogues, on the fp32 (8-bit products: int32) accumulator:
+//   STORE      C rounded to 16 bits
+//   GATE       the tile holds BN / 2 columns of g and the same columns of u (one CTA of the pair loads the gate's weights,
+//              the other the value's): h = act(g) u, and g and u kept for the backward pass
+//   GATE_GRAD  C = dh: dg = dh u act'(g), du = dh act(g)
+//   I8         C scale_a[m] scale_b[n] + bias[n], rounded to the output's type
+// An output whose address and row distance are multiples of 16 bytes leaves through shared memory by TMA stores of 128-byte
+// row pieces; the others are stored element by element.
+#include <string.h>
+
+#include <algorithm>
+
+#include "asd_ops_tc.cuh"
+
+namespace asd {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn();  // asd_gemm.cu
+
+namespace {
+
+constexpr int kStoreBytes = 32 * 128;  // a warp's staging buffer: 32 rows of 128 bytes
+constexpr int kBand = 8;               // tile rows that are walked over together
+
+struct PairMaps {
+  CUtensorMap a[2], b[2], c[2];
+};
+struct PairArgs {
+  int m, n;       // of C (GATE: n = hidden)
+  int kb[2];      // k-blocks of the first and of the second sum (parts)
+  int groups;     // products side by side
+  int tiles_m, tiles_n;
+  int a_mn, b_mn;
+  uint32_t idesc;
+  int out_type;   // asd_type
+  int gelu;
+  int tma_store;
+  void* c[2];
+  int64_t ldc;
+  uint8_t* gu;
+  int gu_cols;    // blocks of 32 columns
+  const float* scale_a;
+  const float* scale_b;
+  const float* bias;
+  int* err;
+};
+
+template <int BN, int EPI>
+struct OpPairCfg {
+  static constexpr int kStageBytes = (BM + BN / 2) * 128;  // per CTA: 128 rows of A, BN / 2 of B, 128 bytes each
+  static constexpr int kBufs = EPI == OPS_GATE_GRAD ? 2 : 1;  // staging buffers of a warp
+  static constexpr int kStages = BN == 256 ? (EPI == OPS_GATE_GRAD ? 5 : 6) : (EPI == OPS_GATE_GRAD ? 6 : 8);
+  static constexpr int kTmemCols = 2 * BN;
+  static constexpr int kSmemBytes = kStages * kStageBytes + kPairEpiWarps * kBufs * kStoreBytes + 1024 + 256;
+  static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
+};
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// A warp's staging buffer, 32 rows of 128 bytes with the 128-byte swizzle of the store's tensor map: 16-byte piece `i` of
+// row `lane`.  Eight neighbouring lanes write eight different pieces of the banks.
+__device__ __forceinline__ void stage_put(uint8_t* buf, int lane, int i, uint4 v) {
+  *reinterpret_cast<uint4*>(buf + lane * 128 + ((i ^ (lane & 7)) << 4)) = v;
+}
+// The buffer may be written again: the store that was issued from it has read it.
+__device__ __forceinline__ void stage_free(int lane) {
+  if (lane == 0) bulk_wait_read();
+  __syncwarp();
+}
+__device__ __forceinline__ void stage_send(const CUtensorMap* map, uint32_t buf, int lane, int x, int y, bool any) {
+  fence_async_shared();
+  __syncwarp();
+  if (lane == 0 && any) {
+    tma_store_2d(map, buf, x, y);
+    bulk_commit();
+  }
+}
+// 32 columns of a row element by element.
+__device__ __forceinline__ void store_row16(void* c, int64_t ldc, int row, int col, int m, int n, const uint32_t (&w)[16]) {
+  if (row >= m) return;
+  uint16_t* p = reinterpret_cast<uint16_t*>(c) + row * ldc + col;
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (col + i < n) p[i] = (uint16_t)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1]);
+}
+__device__ __forceinline__ void store_row32(void* c, int64_t ldc, int row, int col, int m, int n, const float (&f)[32]) {
+  if (row >= m) return;
+  float* p = reinterpret_cast<float*>(c) + row * ldc + col;
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (col + i < n) p[i] = f[i];
+}
+__device__ __forceinline__ void stage_half(uint8_t* buf, int lane, int half, const uint32_t (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) stage_put(buf, lane, 4 * half + i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+}
+
+struct Tile {
+  int group, m0, n0;
+};
+template <int BN>
+__device__ __forceinline__ Tile tile_at(const PairArgs& g, int t) {
+  const int per = g.tiles_m * g.tiles_n;
+  Tile r;
+  r.group = t >= per ? 1 : 0;
+  t -= r.group * per;
+  const int band = t / (kBand * g.tiles_n), first = band * kBand;
+  const int rows = min(g.tiles_m - first, kBand), in = t - first * g.tiles_n;
+  r.m0 = (first + in % rows) * 2 * BM;
+  r.n0 = (in / rows) * BN;
+  return r;
+}
+
+template <int BN, int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ PairArgs g) {
+  using C = OpPairCfg<BN, EPI>;
+  constexpr int S = C::kStages;
+  constexpr bool I8 = EPI == OPS_I8;
+  // columns of C to a tile: half of the accumulator's where it holds g and u
+  constexpr int CN = EPI == OPS_GATE ? BN / 2 : BN;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;
+  uint8_t* stage_ptr = smem_raw + (tiles - raw) + S * C::kStageBytes;
+  uint8_t* aux = stage_ptr + kPairEpiWarps * C::kBufs * kStoreBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(aux);  // full[S], empty[S], acc_full[2], acc_empty[2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aux + 8 * (2 * S + 4));
+  volatile int* dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const uint32_t bar0 = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };
+  auto accf_bar = [&](int b) { return bar0 + 8u * (2 * S + b); };
+  auto acce_bar = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int num_kb = g.kb[0] + g.kb[1];
+  const int n_tiles = g.groups * g.tiles_m * g.tiles_n;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      prefetch_tmap(&maps.a[i]);
+      prefetch_tmap(&maps.b[i]);
+    }
+    for (int s = 0; s < S; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(accf_bar(b), 1);
+      mbar_init(acce_bar(b), 2 * kPairEpiWarps);  // every epilogue warp of both CTAs
+    }
+    *dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"((uint32_t)C::kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  __syncwarp();
+  cluster_sync_all();  // the peer's barriers are initialised before anything arrives on them
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  grid_dependency_wait();
+  grid_launch_dependents();
+
+  if (warp == 0) {
+    // ---------------- TMA producer (both CTAs) ----------------
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int t = pair; t < n_tiles; t += n_pairs) {
+        const Tile tile = tile_at<CN>(g, t);
+        const int m0 = tile.m0 + (int)rank * BM;
+        const int n0 = EPI == OPS_GATE ? tile.n0 : tile.n0 + (int)rank * (BN / 2);
+        for (int kb = 0; kb < num_kb; ++kb) {
+          const int part = kb >= g.kb[0] ? 1 : 0;
+          const int k0 = (kb - part * g.kb[0]) * (I8 ? 128 : 64);
+          const CUtensorMap* ma = &maps.a[part | tile.group];
+          const CUtensorMap* mb = &maps.b[EPI == OPS_GATE ? (int)rank : (part | tile.group)];
+          mbar_wait(empty_bar(stage), phase ^ 1u, dead, g.err);
+          const uint32_t sa = tiles + stage * C::kStageBytes;
+          const uint32_t sb = sa + BM * 128;
+          const uint32_t full0 = map_to_cta(full_bar(stage), 0);
+          if (rank == 0) mbar_expect_tx(full_bar(stage), 2u * (uint32_t)C::kStageBytes);
+          if (!g.a_mn) {
+            tma_load_2d_pair(sa, ma, full0, k0, m0);
+          } else {
+            tma_load_2d_pair(sa, ma, full0, m0, k0);
+            tma_load_2d_pair(sa + 8192, ma, full0, m0 + 64, k0);
+          }
+          if (!g.b_mn) {
+            tma_load_2d_pair(sb, mb, full0, k0, n0);
+          } else {
+#pragma unroll
+            for (int i = 0; i < BN / 128; ++i) tma_load_2d_pair(sb + 8192 * i, mb, full0, n0 + 64 * i, k0);
+          }
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      drain_after_timeout(dead);
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer (rank 0 only) ----------------
+    if (rank == 0 && lane == 0) {
+      const uint64_t step_a = desc_step(g.a_mn), step_b = desc_step(g.b_mn);
+      int stage = 0;
+      uint32_t phase = 0;
+      int it = 0;
+      for (int t = pair; t < n_tiles; t += n_pairs, ++it) {
+        const int acc = it & 1;
+        const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
+        mbar_wait(acce_bar(acc), acc_phase ^ 1u, dead, g.err);  // both CTAs' epilogues have drained it
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
+        for (int kb = 0; kb < num_kb; ++kb) {
+          mbar_wait(full_bar(stage), phase, dead, g.err);
+          tc_fence_after();
+          const uint32_t sa = tiles + stage * C::kStageBytes;
+          const uint64_t da = smem_desc(sa, g.a_mn), db = smem_desc(sa + BM * 128, g.b_mn);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            tc_mma<I8, 2>(d_tmem, da + step_a * k, db + step_b * k, g.idesc, (kb | k) != 0 ? 1u : 0u);
+          tc_commit_pair(empty_bar(stage));                 // frees the stage in this CTA ...
+          tc_commit_pair(map_to_cta(empty_bar(stage), 1));  // ... and in the peer
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        tc_commit_pair(accf_bar(acc));
+        tc_commit_pair(map_to_cta(accf_bar(acc), 1));
+      }
+    }
+  } else {
+    // ---------------- epilogue warps (both CTAs, own 128 rows) ----------------
+    const int quarter = warp & 3;
+    const int half = (warp - kEpiWarp0) >> 2;  // of the tile's columns
+    const bool f16 = g.out_type == ASD_TYPE_F16;
+    const bool gelu = g.gelu != 0;
+    uint8_t* buf = stage_ptr + (warp - kEpiWarp0) * C::kBufs * kStoreBytes;
+    const uint32_t buf_addr = smem_u32(buf);
+    constexpr int kUnits = CN / 64;  // of 64 columns; a tile of one is the first four warps'
+    constexpr int kMine = kUnits >= 2 ? kUnits / 2 : 1;
+    int it = 0;
+    for (int t = pair; t < n_tiles; t += n_pairs, ++it) {
+      const Tile tile = tile_at<CN>(g, t);
+      const int row0 = tile.m0 + (int)rank * BM + quarter * 32;
+      const int row = row0 + lane;
+      const int acc = it & 1;
+      const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
+      const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN);
+      const bool rows_any = row0 < g.m;
+      float sa = 0.f;
+      if (I8 && row < g.m) sa = g.scale_a[row];
+      uint4 kept[2][6];  // GATE_GRAD: g and u of the 32 columns that come next
+      auto fetch_kept = [&](int col) {
+        if (rows_any && col < g.n) {
+          const uint8_t* b = g.gu + gu_block_offset(row0, col, g.gu_cols);
+          gu_fetch(b, lane, kept[0]);
+          gu_fetch(b + kGuHalf, lane, kept[1]);
+        }
+      };
+      if (EPI == OPS_GATE_GRAD) fetch_kept(tile.n0 + half * kMine * 64);
+      mbar_wait(accf_bar(acc), acc_phase, dead, g.err);
+      tc_fence_after();
+      if (half < kUnits) {
+#pragma unroll 1
+        for (int u = 0; u < kMine; ++u) {
+          const int c0 = (half * kMine + u) * 64;  // column in the tile
+          const int col0 = tile.n0 + c0;
+          const bool any = rows_any && col0 < g.n;
+          if (EPI == OPS_STORE || EPI == OPS_GATE) {
+            if (g.tma_store) stage_free(lane);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t w[16];
+              const int col = col0 + 32 * h;
+              if (EPI == OPS_STORE) {
+                uint32_t r[32];
+                tc_ld32(t0 + c0 + 32 * h, r);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = pack16(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]), f16);
+              } else {
+                uint32_t rg[32], ru[32];
+                tc_ld32(t0 + c0 + 32 * h, rg);
+                tc_ld32(t0 + CN + c0 + 32 * h, ru);
+                tc_wait_ld();
+                if (g.gu && rows_any && col < g.n) {
+                  uint8_t* b = g.gu + gu_block_offset(row0, col, g.gu_cols);
+                  gu_store(b, lane, rg);
+                  gu_store(b + kGuHalf, lane, ru);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  const float h0 = gate_value(__uint_as_float(rg[2 * i]), gelu) * __uint_as_float(ru[2 * i]);
+                  const float h1 = gate_value(__uint_as_float(rg[2 * i + 1]), gelu) * __uint_as_float(ru[2 * i + 1]);
+                  w[i] = pack16(h0, h1, f16);
+                }
+              }
+              if (g.tma_store)
+                stage_half(buf, lane, h, w);
+              else
+                store_row16(g.c[tile.group], g.ldc, row, col, g.m, g.n, w);
+            }
+            if (g.tma_store) stage_send(&maps.c[tile.group], buf_addr, lane, col0, row0, any);
+          } else if (EPI == OPS_GATE_GRAD) {
+            stage_free(lane);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t r[32], wg[16], wu[16];
+              tc_ld32(t0 + c0 + 32 * h, r);
+              tc_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float dg[2], du[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  float a, da;
+                  gate_grad(gu_value(kept[0], 2 * i + e), gelu, a, da);
+                  const float dh = __uint_as_float(r[2 * i + e]);
+                  dg[e] = dh * gu_value(kept[1], 2 * i + e) * da;
+                  du[e] = dh * a;
+                }
+                wg[i] = pack16(dg[0], dg[1], f16);
+                wu[i] = pack16(du[0], du[1], f16);
+              }
+              if (h == 0 || u + 1 < kMine) fetch_kept(col0 + 32 * h + 32);
+              stage_half(buf, lane, h, wg);
+              stage_half(buf + kStoreBytes, lane, h, wu);
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0 && any) {
+              tma_store_2d(&maps.c[0], buf_addr, col0, row0);
+              tma_store_2d(&maps.c[1], buf_addr + kStoreBytes, col0, row0);
+              bulk_commit();
+            }
+          } else {
+            const bool f32 = g.out_type == ASD_TYPE_F32;
+            if (g.tma_store) stage_free(lane);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int col = col0 + 32 * h;
+              uint32_t r[32];
+              tc_ld32(t0 + c0 + 32 * h, r);
+              tc_wait_ld();
+              float f[32];
+              // every lane needs the same columns' scales: one load per lane, handed around
+              const int mine = col + lane;
+              const float sb = mine < g.n ? g.scale_b[mine] : 0.f;
+              const float bb = g.bias && mine < g.n ? g.bias[mine] : 0.f;
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                f[i] = fmaf((float)(int)r[i] * sa, __shfl_sync(0xffffffffu, sb, i), __shfl_sync(0xffffffffu, bb, i));
+              if (f32) {
+                if (g.tma_store) {
+                  if (h == 1) stage_free(lane);
+#pragma unroll
+                  for (int i = 0; i < 8; ++i)
+                    stage_put(buf, lane, i, make_uint4(__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]),
+                                                       __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3])));
+                  stage_send(&maps.c[0], buf_addr, lane, col, row0, rows_any && col < g.n);
+                } else {
+                  store_row32(g.c[0], g.ldc, row, col, g.m, g.n, f);
+                }
+              } else {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = pack16(f[2 * i], f[2 * i + 1], f16);
+                if (g.tma_store)
+                  stage_half(buf, lane, h, w);
+                else
+                  store_row16(g.c[0], g.ldc, row, col, g.m, g.n, w);
+              }
+            }
+            if (g.tma_store && !f32) stage_send(&maps.c[0], buf_addr, lane, col0, row0, any);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_cta(acce_bar(acc), 0));
+    }
+    if (lane == 0) bulk_wait_all();  // the stores have left before the CTA does
+  }
+
+  // ---------------- tear-down: neither CTA leaves while the pair's MMAs may still touch it ----------------
+  tc_fence_before();
+  __syncthreads();
+  __syncwarp();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::kTmemCols) : "memory");
+  }
+}
+
+// ---- host side --------------------------------------------------------------------------------
+
+CUtensorMapDataType map_type(int type) {
+  return type == ASD_TYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                              : type == ASD_TYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+}
+// A row-major matrix [rows, cols], boxes of `box_rows` rows of 128 bytes, 128-byte swizzle.
+bool encode(CUtensorMap* out, CUtensorMapDataType dt, int es, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)(ld * es)};
+  cuuint32_t box[2] = {(cuuint32_t)(128 / es), (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(out, dt, 2, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool encode_operand(CUtensorMap* out, const Operand& x, int type, bool i8, int tile_rows) {
+  const CUtensorMapDataType dt = i8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : map_type(type);
+  return encode(out, dt, x.mat.es, x.mat.p, x.mat.rows, x.mat.cols, x.mat.ld, x.mn ? 64 : tile_rows);
+}
+
+template <int BN, int EPI>
+asd_status launch_pair(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
+  using C = OpPairCfg<BN, EPI>;
+  constexpr bool I8 = EPI == OPS_I8;
+  constexpr int CN = EPI == OPS_GATE ? BN / 2 : BN;
+  PairMaps maps;
+  memset(&maps, 0, sizeof(maps));
+  PairArgs g{};
+  const int ke = I8 ? 128 : 64;
+  g.m = (int)q.m, g.n = (int)q.n;
+  g.kb[0] = (int)((q.k[0] + ke - 1) / ke);
+  g.kb[1] = q.parts == 2 ? (int)((q.k[1] + ke - 1) / ke) : 0;
+  g.groups = q.groups;
+  g.tiles_m = (int)((q.m + 2 * BM - 1) / (2 * BM));
+  g.tiles_n = (int)((q.n + CN - 1) / CN);
+  g.a_mn = q.a[0].mn, g.b_mn = q.b[0].mn;
+  const uint32_t fmt = I8 ? 1u : (q.type == ASD_TYPE_BF16 ? 1u : 0u);  // signed 8-bit; bf16 or fp16
+  g.idesc = (I8 ? 2u << 4 : 1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)g.a_mn << 15) | ((uint32_t)g.b_mn << 16) |
+            ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((2 * BM) >> 4) << 24);
+  g.out_type = q.type;
+  g.gelu = q.act == ASD_ACT_GELU;
+  g.ldc = q.ldc;
+  g.gu = q.gu;
+  g.gu_cols = (int)((q.n + 31) / 32);
+  g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias;
+  g.err = o->err;
+  const bool two_b = q.parts == 2 || q.groups == 2 || EPI == OPS_GATE;
+  const int es = ops_type_size(q.type);
+  const int outs = q.groups == 2 || EPI == OPS_GATE_GRAD ? 2 : 1;
+  g.tma_store = 1;
+  for (int i = 0; i < outs; ++i) {
+    g.c[i] = q.c[i];
+    if (((uintptr_t)q.c[i] & 15) || (q.ldc * es) % 16) g.tma_store = 0;
+  }
+  bool ok = true;
+  for (int i = 0; i < 2; ++i) {
+    ok = ok && encode_operand(&maps.a[i], q.a[q.parts == 2 || q.groups == 2 ? i : 0], q.type, I8, BM);
+    ok = ok && encode_operand(&maps.b[i], q.b[two_b ? i : 0], q.type, I8, BN / 2);
+    if (g.tma_store) ok = ok && encode(&maps.c[i], map_type(q.type), es, q.c[i < outs ? i : 0], q.m, q.n, q.ldc, 32);
+  }
+  if (!ok) return ops_fail(ASD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+  const int64_t n_tiles = (int64_t)g.groups * g.tiles_m * g.tiles_n;
+  const int pairs = (int)std::min<int64_t>(n_tiles, o->num_sms / 2);
+  ops_launch(op_pair_kernel<BN, EPI>, dim3(2 * pairs), dim3(kPairThreads), (size_t)C::kSmemBytes, st, 1, maps, g);
+  return ops_launched("matrix product");
+}
+
+// Tile width: the one whose waves of tiles take less time; a tile costs the larger of its MMAs' time and its operands'
+// way into shared memory (a k-block of 128 bytes: 2 BN clocks, 128 (128 + BN / 2) bytes at some 50 bytes a clock).
+template <int EPI>
+asd_status launch_width(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
+  auto cost = [&](int bn) {
+    const int cn = EPI == OPS_GATE ? bn / 2 : bn;
+    const int64_t tiles = (int64_t)q.groups * ((q.m + 2 * BM - 1) / (2 * BM)) * ((q.n + cn - 1) / cn);
+    const int64_t waves = (tiles + o->num_sms / 2 - 1) / (o->num_sms / 2);
+    return (double)waves * std::max(2.0 * bn, (BM + bn / 2) * 128 / 50.0);
+  };
+  return cost(256) <= cost(128) ? launch_pair<256, EPI>(o, q, st) : launch_pair<128, EPI>(o, q, st);
+}
+
+template <int BN, int EPI>
+cudaError_t prepare_pair() {
+  return cudaFuncSetAttribute(op_pair_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, OpPairCfg<BN, EPI>::kSmemBytes);
+}
+
+}  // namespace
+
+int64_t gated_saved_gu_bytes(int64_t rows, int64_t hidden) { return (rows + 31) / 32 * ((hidden + 31) / 32) * kGuBlock; }
+
+asd_status ops_gemm(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
+  switch (q.epi) {
+    case OPS_STORE: return launch_width<OPS_STORE>(o, q, st);
+    case OPS_GATE: return launch_width<OPS_GATE>(o, q, st);
+    case OPS_GATE_GRAD: return launch_width<OPS_GATE_GRAD>(o, q, st);
+    default: return launch_width<OPS_I8>(o, q, st);
+  }
+}
+
+asd_status ops_gemm_prepare() {
+  const cudaError_t all[] = {prepare_pair<256, OPS_STORE>(),     prepare_pair<128, OPS_STORE>(), prepare_pair<256, OPS_GATE>(),
+                             prepare_pair<128, OPS_GATE>(),      prepare_pair<256, OPS_GATE_GRAD>(),
+                             prepare_pair<128, OPS_GATE_GRAD>(), prepare_pair<256, OPS_I8>(),    prepare_pair<128, OPS_I8>()};
+  for (cudaError_t e : all)
+    if (e != cudaSuccess) return ops_fail(ASD_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+  return ASD_OK;
+}
+
+}  // namespace asd

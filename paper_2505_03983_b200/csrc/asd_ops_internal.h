@@ -1,0 +1,93 @@
+// Internal declarations shared by the translation units of the operators (include/asd_ops.h): the handle, the
+// message of a failed call, and the launchers of the kernels.  Nothing here crosses the C ABI.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "asd_ops.h"
+
+struct asd_ops {
+  int device;
+  int num_sms;
+  int* err;  // device word: 0, or ASD_ERR_TIMEOUT
+};
+
+namespace asd {
+
+constexpr int kOpsMaxDim = 1 << 24;  // rows' lengths; keeps a row's products of sizes inside 32 bits
+constexpr int kOpsMaxK8 = 131071;    // 2^31 / 128^2: the longest sum of 8-bit products that int32 holds
+
+asd_status ops_fail(asd_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+asd_status ops_launched(const char* what);  // OK, or CUDA with the launch's error
+int ops_type_size(int type);                // bytes of an asd_type, 0 if it is none
+
+// Launch with programmatic stream serialization: the kernel may start while its predecessor in the stream ends; every
+// kernel of this library waits for it (griddepcontrol.wait) before it touches global memory.
+template <typename... P, typename... A>
+inline void ops_launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, int cluster, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cluster > 1) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+  }
+  cudaLaunchKernelEx(&cfg, kernel, P(args)...);  // its status is read by ops_launched
+}
+
+// A matrix operand: `rows` rows of `cols` contiguous elements, `ld` elements apart.
+struct Mat {
+  const void* p;
+  int64_t rows, cols, ld;
+  int es;  // bytes of an element
+};
+inline bool mat_aligned(const Mat& m) { return ((uintptr_t)m.p & 15) == 0 && (m.ld * m.es) % 16 == 0; }
+
+// ---- asd_ops_rows.cu: one row at a time -------------------------------------------------------------
+void launch_rmsnorm(const asd_ops* o, const asd_rmsnorm_args* a, cudaStream_t st);
+int64_t rmsnorm_backward_bytes(const asd_ops* o, const asd_rmsnorm_backward_args* a);
+void launch_rmsnorm_backward(const asd_ops* o, const asd_rmsnorm_backward_args* a, cudaStream_t st);
+void launch_quantize(const asd_ops* o, const asd_quantize_args* a, cudaStream_t st);
+void launch_pack(const asd_ops* o, const Mat& src, void* dst, int64_t ld_dst, cudaStream_t st);
+
+// ---- asd_ops_gemm.cu: matrix products -----------------------------------------------------------------
+// C[m, n] = sum_k A(m, k) B(n, k).  An operand is read either as a row-major matrix [its m or n, k] or, `mn` true, as
+// the transpose of a row-major matrix [k, its m or n].
+struct Operand {
+  Mat mat;
+  bool mn;
+};
+enum OpsEpi { OPS_STORE = 0, OPS_GATE = 1, OPS_GATE_GRAD = 2, OPS_I8 = 3 };
+struct OpsGemm {
+  int epi;
+  int type;    // asd_type of the 16-bit operands and outputs (OPS_I8: of the output)
+  int act;     // OPS_GATE, OPS_GATE_GRAD
+  int64_t m, n, k[2];
+  int parts;   // OPS_STORE: 1, or 2 sums over k one after the other (k[0] of a[0], b[0], then k[1] of a[1], b[1])
+  int groups;  // OPS_STORE: 1, or 2 products side by side (a[g], b[g] -> c[g])
+  Operand a[2], b[2];  // OPS_GATE: b[0] the gate's weights, b[1] the value's
+  void* c[2];          // outputs; OPS_GATE: c[0] = h; OPS_GATE_GRAD: c[0] = dg, c[1] = du
+  int64_t ldc;
+  uint8_t* gu;         // OPS_GATE: where g and u are kept, or NULL; OPS_GATE_GRAD: where they were
+  const float* scale_a;  // OPS_I8
+  const float* scale_b;
+  const float* bias;
+};
+int64_t gated_saved_gu_bytes(int64_t rows, int64_t hidden);
+asd_status ops_gemm(const asd_ops* o, const OpsGemm& g, cudaStream_t st);
+asd_status ops_gemm_prepare();  // per device: opt-in to large shared memory
+
+}  // namespace asd

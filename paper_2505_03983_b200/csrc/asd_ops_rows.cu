@@ -1,0 +1,651 @@
+// Operators that work on one row at a time: s = x + r with its root-mean-square norm (16 / 32 bits, or 8 bits with a scale
+// per row), the norm's gradients, the row quantisation with or without the gate, and the copy that aligns an operand of a
+// matrix product.
+//
+// All of them are bound by memory: a row is read once, kept in registers over its reductions, and written once.  A row
+// belongs to 32, 128 or 512 threads (rows of up to 1024, 4096, 16384), 32 elements to a thread, so that a thread has its
+// 16-byte loads in flight together; longer rows are read a second time.  A row whose address, distance or length is not a
+// multiple of 8 elements is read element by element, neighbouring threads on neighbouring elements.
+#include <float.h>
+
+#include "asd_ops_internal.h"
+
+namespace asd {
+namespace {
+
+constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: the least magnitude that a row's scale is made from
+constexpr int kPer = 32;                         // elements of a row that one thread keeps
+
+__device__ __forceinline__ void dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename T>
+__device__ __forceinline__ float to_f(T v);
+template <>
+__device__ __forceinline__ float to_f<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f<__half>(__half v) { return __half2float(v); }
+template <>
+__device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T from_f(float v);
+template <>
+__device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// VEC = 8 or 1 neighbouring elements; VEC = 8 asks for 16-byte aligned addresses (8 for int8).
+template <int VEC, typename T>
+__device__ __forceinline__ void load_vec(const T* p, float (&f)[VEC]) {
+  if constexpr (VEC == 1) {
+    f[0] = to_f<T>(*p);
+  } else if constexpr (sizeof(T) == 4) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  } else {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const T* e = reinterpret_cast<const T*>(&v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = to_f<T>(e[i]);
+  }
+}
+template <int VEC, typename T>
+__device__ __forceinline__ void store_vec(T* p, const float (&f)[VEC]) {
+  if constexpr (VEC == 1) {
+    *p = from_f<T>(f[0]);
+  } else if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  } else {
+    uint4 v;
+    T* e = reinterpret_cast<T*>(&v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = from_f<T>(f[i]);
+    *reinterpret_cast<uint4*>(p) = v;
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void store_q(int8_t* p, const float (&f)[VEC], float inv) {
+  if constexpr (VEC == 1) {
+    *p = (int8_t)__float2int_rn(f[0] * inv);
+  } else {
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b[i] = (uint32_t)__float2int_rn(f[4 * h + i] * inv) & 0xffu;
+      w[h] = b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24);
+    }
+    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  }
+}
+template <int VEC, typename T>
+__device__ __forceinline__ void load_weight(const void* w, int w_f32, int col, float (&f)[VEC]) {
+  if (!w) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) f[i] = 1.f;
+  } else if (w_f32) {
+    load_vec<VEC, float>(reinterpret_cast<const float*>(w) + col, f);
+  } else {
+    load_vec<VEC, T>(reinterpret_cast<const T*>(w) + col, f);
+  }
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// Sum and largest over the threads of a row (a warp, or the block).  `buf`: one word per warp; a block's call ends with
+// the buffer free for the next one after another barrier, so alternate two buffers.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* buf) {
+  v = warp_sum(v);
+  if (TPR == 32) return v;
+  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+  __syncthreads();
+  float t = 0.f;
+#pragma unroll
+  for (int i = 0; i < TPR / 32; ++i) t += buf[i];
+  return t;
+}
+template <int TPR>
+__device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* buf) {
+  v = __reduce_max_sync(0xffffffffu, v);
+  if (TPR == 32) return v;
+  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+  __syncthreads();
+  uint32_t t = 0;
+#pragma unroll
+  for (int i = 0; i < TPR / 32; ++i) t = max(t, buf[i]);
+  return t;
+}
+// Magnitudes are compared as their bit patterns: the order of the numbers, with infinity above all of them and NaN above
+// infinity, so that one maximum also tells whether the row can be represented.
+__device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+struct RowScale {
+  float inv, scale;  // q = rint(y inv), y ~ q scale
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t most) {
+  if (most >= 0x7f800000u) return {0.f, __uint_as_float(0x7fffffffu)};
+  const float m = fmaxf(__uint_as_float(most), kTiny);
+  return {127.f / m, m / 127.f};
+}
+
+__device__ __forceinline__ float act_value(float g, int act) {
+  if (act == ASD_ACT_SILU) return g * (1.f / (1.f + __expf(-g)));
+  return 0.5f * g * (1.f + erff(g * 0.7071067811865476f));
+}
+
+struct NormArgs {
+  int rows, width, w_f32;
+  float eps;
+  const void *x, *r, *w;
+  void *sum, *y;
+  float* scale;
+  int64_t ld_x, ld_r, ld_s, ld_y;
+};
+
+// Threads of a block: the row's, or four rows of a warp each.
+template <int TPR>
+constexpr int block_of = TPR == 32 ? 128 : TPR;
+
+// s and its norm.  TPR threads to a row, kPer elements each (LONG: any number, s read back or added up again for the
+// second pass).
+template <typename T, int VEC, int TPR, bool Q8, bool LONG>
+__global__ void __launch_bounds__(block_of<TPR>) rmsnorm_kernel(const NormArgs a) {
+  constexpr int NV = kPer / VEC;
+  __shared__ float buf_s[TPR / 32];
+  __shared__ uint32_t buf_m[TPR / 32];
+  dep_wait();
+  dep_launch();
+  const int t = TPR == 32 ? (threadIdx.x & 31) : threadIdx.x;
+  const int row = TPR == 32 ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+  if (row >= a.rows) return;  // whole warps: rows of a block do not share a barrier
+  const T* x = reinterpret_cast<const T*>(a.x) + row * a.ld_x;
+  const T* r = a.r ? reinterpret_cast<const T*>(a.r) + row * a.ld_r : nullptr;
+  T* so = a.sum ? reinterpret_cast<T*>(a.sum) + row * a.ld_s : nullptr;
+  auto fetch = [&](int col, float(&f)[VEC]) {  // the rounded s
+    load_vec<VEC, T>(x + col, f);
+    if (r) {
+      float g[VEC];
+      load_vec<VEC, T>(r + col, g);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f[i] = to_f<T>(from_f<T>(f[i] + g[i]));
+    }
+  };
+  if constexpr (!LONG) {
+    float f[NV][VEC];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width)
+        fetch(col, f[v]);
+      else
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[v][i] = 0.f;
+    }
+    float sq = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (so && col < a.width) store_vec<VEC, T>(so + col, f[v]);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) sq = fmaf(f[v][i], f[v][i], sq);
+    }
+    sq = row_sum<TPR>(sq, buf_s);
+    const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
+    uint32_t most = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) {
+        float w[VEC];
+        load_weight<VEC, T>(a.w, a.w_f32, col, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          f[v][i] = f[v][i] * rho * w[i];
+          if (Q8) most = max(most, mag(f[v][i]));
+        }
+        if (!Q8) store_vec<VEC, T>(reinterpret_cast<T*>(a.y) + row * a.ld_y + col, f[v]);
+      }
+    }
+    if (Q8) {
+      const RowScale rs = row_scale(row_max<TPR>(most, buf_m));
+      int8_t* y = reinterpret_cast<int8_t*>(a.y) + row * a.ld_y;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int col = (v * TPR + t) * VEC;
+        if (col < a.width) store_q<VEC>(y + col, f[v], rs.inv);
+      }
+      if (t == 0) a.scale[row] = rs.scale;
+    }
+  } else {
+    float sq = 0.f;
+    for (int col = t * VEC; col < a.width; col += TPR * VEC) {
+      float f[VEC];
+      fetch(col, f);
+      if (so) store_vec<VEC, T>(so + col, f);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) sq = fmaf(f[i], f[i], sq);
+    }
+    sq = row_sum<TPR>(sq, buf_s);
+    const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
+    // s once more: from where this thread has stored it (x or r may be gone by now), or added up again
+    auto again = [&](int col, float(&f)[VEC]) {
+      if (so)
+        load_vec<VEC, T>(so + col, f);
+      else
+        fetch(col, f);
+      float w[VEC];
+      load_weight<VEC, T>(a.w, a.w_f32, col, w);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f[i] = f[i] * rho * w[i];
+    };
+    uint32_t most = 0;
+    for (int col = t * VEC; col < a.width; col += TPR * VEC) {
+      float f[VEC];
+      again(col, f);
+      if (Q8) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) most = max(most, mag(f[i]));
+      } else {
+        store_vec<VEC, T>(reinterpret_cast<T*>(a.y) + row * a.ld_y + col, f);
+      }
+    }
+    if (Q8) {
+      const RowScale rs = row_scale(row_max<TPR>(most, buf_m));
+      for (int col = t * VEC; col < a.width; col += TPR * VEC) {
+        float f[VEC];
+        again(col, f);
+        store_q<VEC>(reinterpret_cast<int8_t*>(a.y) + row * a.ld_y + col, f, rs.inv);
+      }
+      if (t == 0) a.scale[row] = rs.scale;
+    }
+  }
+}
+
+struct QuantArgs {
+  int rows, width, act;
+  const void* x;
+  int8_t* q;
+  float* scale;
+  int64_t ld_x, ld_q;
+};
+
+template <typename T, int VEC, int TPR, bool LONG>
+__global__ void __launch_bounds__(block_of<TPR>) quantize_kernel(const QuantArgs a) {
+  constexpr int NV = kPer / VEC;
+  __shared__ uint32_t buf_m[TPR / 32];
+  dep_wait();
+  dep_launch();
+  const int t = TPR == 32 ? (threadIdx.x & 31) : threadIdx.x;
+  const int row = TPR == 32 ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+  if (row >= a.rows) return;
+  const T* x = reinterpret_cast<const T*>(a.x) + row * a.ld_x;
+  int8_t* q = a.q + row * a.ld_q;
+  auto fetch = [&](int col, float(&f)[VEC]) {
+    load_vec<VEC, T>(x + col, f);
+    if (a.act != ASD_ACT_NONE) {
+      float u[VEC];
+      load_vec<VEC, T>(x + a.width + col, u);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f[i] = act_value(f[i], a.act) * u[i];
+    }
+  };
+  uint32_t most = 0;
+  if constexpr (!LONG) {
+    float f[NV][VEC];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) {
+        fetch(col, f[v]);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) most = max(most, mag(f[v][i]));
+      }
+    }
+    const RowScale rs = row_scale(row_max<TPR>(most, buf_m));
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) store_q<VEC>(q + col, f[v], rs.inv);
+    }
+    if (t == 0) a.scale[row] = rs.scale;
+  } else {
+    for (int col = t * VEC; col < a.width; col += TPR * VEC) {
+      float f[VEC];
+      fetch(col, f);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) most = max(most, mag(f[i]));
+    }
+    const RowScale rs = row_scale(row_max<TPR>(most, buf_m));
+    for (int col = t * VEC; col < a.width; col += TPR * VEC) {
+      float f[VEC];
+      fetch(col, f);
+      store_q<VEC>(q + col, f, rs.inv);
+    }
+    if (t == 0) a.scale[row] = rs.scale;
+  }
+}
+
+struct NormGradArgs {
+  int rows, width, w_f32, blocks;
+  float eps;
+  const void *dy, *s, *ds, *w;
+  void* dx;
+  float* part;  // [blocks, width] sums of dy z over a block's rows, or NULL
+  float* rho;   // LONG: [rows]
+  int64_t ld_dy, ld_s, ld_ds, ld_dx;
+};
+
+// Gradients.  One block walks over rows blockIdx.x, + blocks, ...; a thread keeps the same columns in every row, so the
+// sums of dw over the block's rows stay in its registers and are written once, to be added up by reduce_dw_kernel.  Both
+// sums of a row, of s^2 and of dy w s, are taken together: mean(dy w z) = rho mean(dy w s).
+template <typename T, int VEC, int TPR, int PER>
+__global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a) {
+  constexpr int NV = PER / VEC;
+  __shared__ float buf[2][2][TPR / 32];
+  dep_wait();
+  dep_launch();
+  const int t = threadIdx.x;
+  float acc[NV][VEC];
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[v][i] = 0.f;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks, turn ^= 1) {
+    const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.ld_dy;
+    const T* s = reinterpret_cast<const T*>(a.s) + row * a.ld_s;
+    float g[NV][VEC], f[NV][VEC];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) {
+        load_vec<VEC, T>(s + col, f[v]);
+        load_vec<VEC, T>(dy + col, g[v]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[v][i] = g[v][i] = 0.f;
+      }
+    }
+    float sq = 0.f, dot = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) {
+        float w[VEC];
+        load_weight<VEC, T>(a.w, a.w_f32, col, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          sq = fmaf(f[v][i], f[v][i], sq);
+          dot = fmaf(g[v][i] * w[i], f[v][i], dot);
+        }
+      }
+    }
+    sq = warp_sum(sq);
+    dot = warp_sum(dot);
+    if ((t & 31) == 0) {
+      buf[turn][0][t >> 5] = sq;
+      buf[turn][1][t >> 5] = dot;
+    }
+    __syncthreads();
+    sq = dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < TPR / 32; ++i) {
+      sq += buf[turn][0][i];
+      dot += buf[turn][1][i];
+    }
+    const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
+    const float c = rho * dot / (float)a.width;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) {
+        float w[VEC], d[VEC], e[VEC];
+        load_weight<VEC, T>(a.w, a.w_f32, col, w);
+        if (a.ds) load_vec<VEC, T>(reinterpret_cast<const T*>(a.ds) + row * a.ld_ds + col, e);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float z = f[v][i] * rho;
+          acc[v][i] = fmaf(g[v][i], z, acc[v][i]);
+          d[i] = rho * (g[v][i] * w[i] - z * c);
+          if (a.ds) d[i] += e[i];
+        }
+        if (a.dx) store_vec<VEC, T>(reinterpret_cast<T*>(a.dx) + row * a.ld_dx + col, d);
+      }
+    }
+  }
+  if (a.part) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) a.part[(size_t)blockIdx.x * a.width + col + i] = acc[v][i];
+      }
+    }
+  }
+}
+
+// Rows of more than 16384: dx row by row with rho kept per row, the sums of dw by columns afterwards.
+template <typename T>
+__global__ void __launch_bounds__(512) rmsnorm_grad_long_kernel(const NormGradArgs a) {
+  __shared__ float buf[2][16];
+  dep_wait();
+  dep_launch();
+  const int t = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.ld_dy;
+  const T* s = reinterpret_cast<const T*>(a.s) + row * a.ld_s;
+  float sq = 0.f, dot = 0.f, w[1], f[1], g[1];
+  for (int col = t; col < a.width; col += 512) {
+    load_vec<1, T>(s + col, f);
+    load_vec<1, T>(dy + col, g);
+    load_weight<1, T>(a.w, a.w_f32, col, w);
+    sq = fmaf(f[0], f[0], sq);
+    dot = fmaf(g[0] * w[0], f[0], dot);
+  }
+  sq = row_sum<512>(sq, buf[0]);
+  dot = row_sum<512>(dot, buf[1]);
+  const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
+  const float c = rho * dot / (float)a.width;
+  if (t == 0 && a.rho) a.rho[row] = rho;
+  if (!a.dx) return;
+  for (int col = t; col < a.width; col += 512) {
+    load_vec<1, T>(s + col, f);
+    load_vec<1, T>(dy + col, g);
+    load_weight<1, T>(a.w, a.w_f32, col, w);
+    float d = rho * (g[0] * w[0] - f[0] * rho * c);
+    if (a.ds) d += to_f<T>(reinterpret_cast<const T*>(a.ds)[row * a.ld_ds + col]);
+    reinterpret_cast<T*>(a.dx)[row * a.ld_dx + col] = from_f<T>(d);
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(128) columns_dw_kernel(const NormGradArgs a) {
+  dep_wait();
+  dep_launch();
+  const int col = blockIdx.x * 128 + threadIdx.x;
+  if (col >= a.width) return;
+  float acc = 0.f;
+  for (int64_t row = blockIdx.y; row < a.rows; row += a.blocks)
+    acc = fmaf(to_f<T>(reinterpret_cast<const T*>(a.dy)[row * a.ld_dy + col]),
+               to_f<T>(reinterpret_cast<const T*>(a.s)[row * a.ld_s + col]) * a.rho[row], acc);
+  a.part[(size_t)blockIdx.y * a.width + col] = acc;
+}
+
+// dw[col] = sum over blocks of part[block, col], in a fixed order: 32 columns to a block, 32 threads to a column.
+template <typename W>
+__global__ void __launch_bounds__(1024) reduce_dw_kernel(const float* part, int blocks, int width, W* dw) {
+  __shared__ float buf[32][33];
+  dep_wait();
+  dep_launch();
+  const int col = blockIdx.x * 32 + threadIdx.x;
+  float acc = 0.f;
+  if (col < width)
+    for (int b = threadIdx.y; b < blocks; b += 32) acc += part[(size_t)b * width + col];
+  buf[threadIdx.y][threadIdx.x] = acc;
+  __syncthreads();
+  const float v = warp_sum(buf[threadIdx.x][threadIdx.y]);
+  if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < width) dw[blockIdx.x * 32 + threadIdx.y] = from_f<W>(v);
+}
+
+// Rows of `cols` elements, ld_src apart, to rows ld_dst apart.
+template <typename E>
+__global__ void __launch_bounds__(256) pack_rows_kernel(const E* src, int64_t ld_src, int64_t rows, int cols, E* dst, int64_t ld_dst) {
+  dep_wait();
+  dep_launch();
+  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y)
+    for (int col = blockIdx.x * 256 + threadIdx.x; col < cols; col += gridDim.x * 256)
+      dst[row * ld_dst + col] = src[row * ld_src + col];
+}
+
+bool aligned(const void* p, int64_t ld, int es, int bytes) { return ((uintptr_t)p % bytes) == 0 && (ld * es) % bytes == 0; }
+
+// Threads to a row.  A row of up to 1024 is a warp's, so that its sums need no barrier, unless there are too few rows to
+// fill the SMs with warps; then, and beyond, a block's.
+int row_threads(const asd_ops* o, int64_t rows, int width) {
+  if (width <= 32 * kPer && (width <= 256 || rows >= 8 * o->num_sms)) return 32;
+  if (width <= 128 * kPer && (width <= 1024 || rows >= 4 * o->num_sms)) return 128;
+  return 512;
+}
+
+template <typename T, int VEC, bool Q8>
+void rmsnorm_t(const asd_ops* o, const NormArgs& n, cudaStream_t st) {
+  const int tpr = row_threads(o, n.rows, n.width);
+  if (tpr == 32)
+    ops_launch(rmsnorm_kernel<T, VEC, 32, Q8, false>, dim3((n.rows + 3) / 4), dim3(128), 0, st, 1, n);
+  else if (tpr == 128)
+    ops_launch(rmsnorm_kernel<T, VEC, 128, Q8, false>, dim3(n.rows), dim3(128), 0, st, 1, n);
+  else if (n.width <= 512 * kPer)
+    ops_launch(rmsnorm_kernel<T, VEC, 512, Q8, false>, dim3(n.rows), dim3(512), 0, st, 1, n);
+  else
+    ops_launch(rmsnorm_kernel<T, VEC, 512, Q8, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
+}
+template <typename T>
+void rmsnorm_type(const asd_ops* o, const NormArgs& n, bool vec, bool q8, cudaStream_t st) {
+  if (vec)
+    q8 ? rmsnorm_t<T, 8, true>(o, n, st) : rmsnorm_t<T, 8, false>(o, n, st);
+  else
+    q8 ? rmsnorm_t<T, 1, true>(o, n, st) : rmsnorm_t<T, 1, false>(o, n, st);
+}
+
+template <typename T, int VEC>
+void quantize_t(const asd_ops* o, const QuantArgs& n, cudaStream_t st) {
+  const int tpr = row_threads(o, n.rows, n.width);
+  if (tpr == 32)
+    ops_launch(quantize_kernel<T, VEC, 32, false>, dim3((n.rows + 3) / 4), dim3(128), 0, st, 1, n);
+  else if (tpr == 128)
+    ops_launch(quantize_kernel<T, VEC, 128, false>, dim3(n.rows), dim3(128), 0, st, 1, n);
+  else if (n.width <= 512 * kPer)
+    ops_launch(quantize_kernel<T, VEC, 512, false>, dim3(n.rows), dim3(512), 0, st, 1, n);
+  else
+    ops_launch(quantize_kernel<T, VEC, 512, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
+}
+
+// Blocks of the gradient: enough to fill the SMs, few enough that their partial sums of dw stay a small share of the
+// traffic.
+int grad_blocks(const asd_ops* o, int64_t rows, int width) {
+  const int per_sm = width <= 1024 ? 8 : width <= 4096 ? 3 : width <= 16384 ? 1 : 2;
+  const int64_t most = (int64_t)per_sm * o->num_sms;
+  return (int)(rows < most ? rows : most);
+}
+template <typename T, int VEC>
+void grad_t(const asd_ops* o, const NormGradArgs& n, cudaStream_t st) {
+  if (n.width <= 1024)
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 64, 16>, dim3(n.blocks), dim3(64), 0, st, 1, n);
+  else if (n.width <= 4096)
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 256, 16>, dim3(n.blocks), dim3(256), 0, st, 1, n);
+  else if (n.width <= 16384)
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 512, 32>, dim3(n.blocks), dim3(512), 0, st, 1, n);
+  else {
+    ops_launch(rmsnorm_grad_long_kernel<T>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    if (n.part) ops_launch(columns_dw_kernel<T>, dim3((n.width + 127) / 128, n.blocks), dim3(128), 0, st, 1, n);
+  }
+}
+
+}  // namespace
+
+void launch_rmsnorm(const asd_ops* o, const asd_rmsnorm_args* a, cudaStream_t st) {
+  NormArgs n{};
+  n.rows = a->rows, n.width = a->width, n.w_f32 = a->w_type == ASD_TYPE_F32, n.eps = a->eps;
+  n.x = a->x, n.r = a->residual, n.w = a->weight, n.sum = a->sum, n.y = a->y, n.scale = a->scale;
+  n.ld_x = a->ld_x, n.ld_r = a->ld_residual, n.ld_s = a->ld_sum, n.ld_y = a->ld_y;
+  const int es = ops_type_size(a->type);
+  const bool q8 = a->scale != nullptr;
+  const bool vec = a->width % 8 == 0 && aligned(a->x, a->ld_x, es, 16) && (!a->residual || aligned(a->residual, a->ld_residual, es, 16)) &&
+                   (!a->weight || aligned(a->weight, 0, es, 16)) && (!a->sum || aligned(a->sum, a->ld_sum, es, 16)) &&
+                   (q8 ? aligned(a->y, a->ld_y, 1, 8) : aligned(a->y, a->ld_y, es, 16));
+  if (a->type == ASD_TYPE_F32)
+    rmsnorm_type<float>(o, n, vec, q8, st);
+  else if (a->type == ASD_TYPE_F16)
+    rmsnorm_type<__half>(o, n, vec, q8, st);
+  else
+    rmsnorm_type<__nv_bfloat16>(o, n, vec, q8, st);
+}
+
+void launch_quantize(const asd_ops* o, const asd_quantize_args* a, cudaStream_t st) {
+  QuantArgs n{};
+  n.rows = a->rows, n.width = a->width, n.act = a->act, n.x = a->x, n.q = a->q, n.scale = a->scale, n.ld_x = a->ld_x, n.ld_q = a->ld_q;
+  const bool vec = a->width % 8 == 0 && aligned(a->x, a->ld_x, ops_type_size(a->type), 16) && aligned(a->q, a->ld_q, 1, 8);
+  if (a->type == ASD_TYPE_F32)
+    vec ? quantize_t<float, 8>(o, n, st) : quantize_t<float, 1>(o, n, st);
+  else if (a->type == ASD_TYPE_F16)
+    vec ? quantize_t<__half, 8>(o, n, st) : quantize_t<__half, 1>(o, n, st);
+  else
+    vec ? quantize_t<__nv_bfloat16, 8>(o, n, st) : quantize_t<__nv_bfloat16, 1>(o, n, st);
+}
+
+int64_t rmsnorm_backward_bytes(const asd_ops* o, const asd_rmsnorm_backward_args* a) {
+  if (!a->dw || a->rows == 0) return 0;
+  return 4 * ((int64_t)grad_blocks(o, a->rows, a->width) * a->width + (a->width > 16384 ? a->rows : 0));
+}
+
+void launch_rmsnorm_backward(const asd_ops* o, const asd_rmsnorm_backward_args* a, cudaStream_t st) {
+  NormGradArgs n{};
+  n.rows = a->rows, n.width = a->width, n.w_f32 = a->w_type == ASD_TYPE_F32, n.eps = a->eps;
+  n.blocks = grad_blocks(o, a->rows, a->width);
+  n.dy = a->dy, n.s = a->s, n.ds = a->ds, n.w = a->weight, n.dx = a->dx;
+  n.ld_dy = a->ld_dy, n.ld_s = a->ld_s, n.ld_ds = a->ld_ds, n.ld_dx = a->ld_dx;
+  if (a->dw) {
+    n.part = reinterpret_cast<float*>(a->workspace);
+    n.rho = n.part + (size_t)n.blocks * a->width;
+  }
+  const int es = ops_type_size(a->type);
+  const bool vec = a->width % 8 == 0 && aligned(a->dy, a->ld_dy, es, 16) && aligned(a->s, a->ld_s, es, 16) &&
+                   (!a->ds || aligned(a->ds, a->ld_ds, es, 16)) && (!a->weight || aligned(a->weight, 0, es, 16)) &&
+                   (!a->dx || aligned(a->dx, a->ld_dx, es, 16));
+  if (a->type == ASD_TYPE_F32)
+    vec ? grad_t<float, 8>(o, n, st) : grad_t<float, 1>(o, n, st);
+  else if (a->type == ASD_TYPE_F16)
+    vec ? grad_t<__half, 8>(o, n, st) : grad_t<__half, 1>(o, n, st);
+  else
+    vec ? grad_t<__nv_bfloat16, 8>(o, n, st) : grad_t<__nv_bfloat16, 1>(o, n, st);
+  if (!a->dw) return;
+  const dim3 grid((a->width + 31) / 32), block(32, 32);
+  if (a->w_type == ASD_TYPE_F32)
+    ops_launch(reduce_dw_kernel<float>, grid, block, 0, st, 1, (const float*)n.part, n.blocks, n.width, reinterpret_cast<float*>(a->dw));
+  else if (a->w_type == ASD_TYPE_F16)
+    ops_launch(reduce_dw_kernel<__half>, grid, block, 0, st, 1, (const float*)n.part, n.blocks, n.width, reinterpret_cast<__half*>(a->dw));
+  else
+    ops_launch(reduce_dw_kernel<__nv_bfloat16>, grid, block, 0, st, 1, (const float*)n.part, n.blocks, n.width,
+               reinterpret_cast<__nv_bfloat16*>(a->dw));
+}
+
+void launch_pack(const asd_ops* o, const Mat& src, void* dst, int64_t ld_dst, cudaStream_t st) {
+  const int bx = (int)((src.cols + 255) / 256 < 64 ? (src.cols + 255) / 256 : 64);
+  int64_t by = (int64_t)o->num_sms * 16 / bx;
+  if (by > src.rows) by = src.rows;
+  if (by < 1) by = 1;
+  const dim3 grid(bx, (unsigned)by);
+  if (src.es == 1)
+    ops_launch(pack_rows_kernel<uint8_t>, grid, dim3(256), 0, st, 1, (const uint8_t*)src.p, src.ld, src.rows, (int)src.cols, (uint8_t*)dst, ld_dst);
+  else
+    ops_launch(pack_rows_kernel<uint16_t>, grid, dim3(256), 0, st, 1, (const uint16_t*)src.p, src.ld, src.rows, (int)src.cols, (uint16_t*)dst, ld_dst);
+}
+
+}  // namespace asd

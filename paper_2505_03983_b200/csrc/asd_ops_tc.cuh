@@ -1,0 +1,139 @@
+// Device-side pieces shared by the operators' tensor-core kernels: shared-memory descriptors of both operand orders, the
+// MMA of each operand kind, the gated activation with its gradient, and the 24-bit form in which a training step keeps
+// the two projections.  Everything here has internal linkage.
+#pragma once
+
+#include "asd_ops_internal.h"
+#include "asd_tc.cuh"
+
+namespace asd {
+namespace {
+
+// A tile in shared memory is made of 128-byte rows with the 128-byte swizzle, as the TMA writes them.
+//   along k:  a row is an m or n index, 64 16-bit (128 8-bit) elements of k; groups of 8 rows are 1024 bytes apart
+//             (stride offset).  One MMA's k is 32 bytes of a row: the next starts 32 bytes further.
+//   along mn: a row is a k index, 64 elements of m or n; groups of 8 rows are 1024 bytes apart (stride offset) and
+//             blocks of 64 elements of m or n are 64 rows = 8192 bytes apart (leading offset).  One MMA's k is 16
+//             rows: the next starts 2048 bytes further.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn) {
+  uint64_t d = smem_desc_sw128(addr);
+  if (mn) d = (d & ~(0x3FFFull << 16)) | ((uint64_t)(8192 >> 4) << 16);
+  return d;
+}
+__device__ __forceinline__ uint64_t desc_step(bool mn) { return mn ? 128u : 2u; }
+
+template <bool I8, int CTAS>
+__device__ __forceinline__ void tc_mma(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (!I8 && CTAS == 2)
+    tc_mma_bf16_pair(d_tmem, a, b, idesc, accumulate);
+  else if constexpr (!I8)
+    tc_mma_bf16(d_tmem, a, b, idesc, accumulate);
+  else if constexpr (CTAS == 2)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n\t}" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+        : "memory");
+}
+
+// Two fp32 values rounded to a pair of 16-bit ones, the first in the low half.
+__device__ __forceinline__ uint32_t pack16(float a, float b, bool f16) {
+  uint32_t r;
+  if (f16)
+    asm("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(r) : "f"(a), "f"(b));
+  else
+    asm("cvt.rn.bf16x2.f32 %0, %2, %1;" : "=r"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint16_t round16(float a, bool f16) {
+  return f16 ? __half_as_ushort(__float2half_rn(a)) : __bfloat16_as_ushort(__float2bfloat16_rn(a));
+}
+
+// act(g).  The exponential and reciprocal are the approximate instructions (relative error some 2^-22, far below the
+// 16-bit rounding that follows).
+__device__ __forceinline__ float sigmoid_approx(float g) { return rcp_approx(1.f + ex2_approx(g * kNegLog2e)); }
+__device__ __forceinline__ float gate_value(float g, bool gelu) {
+  if (!gelu) return g * sigmoid_approx(g);
+  return 0.5f * g * (1.f + erff(g * 0.7071067811865476f));
+}
+// act(g) and act'(g):  silu' = p (1 + g (1 - p)),  gelu' = Phi + g phi.
+__device__ __forceinline__ void gate_grad(float g, bool gelu, float& a, float& da) {
+  if (!gelu) {
+    const float p = sigmoid_approx(g);
+    a = g * p;
+    da = fmaf(a, 1.f - p, p);
+  } else {
+    const float p = 0.5f * (1.f + erff(g * 0.7071067811865476f));
+    a = g * p;
+    da = fmaf(g * 0.3989422804014327f, ex2_approx(g * g * -0.7213475204444817f), p);
+  }
+}
+
+// g and u between the forward and the backward pass.  Rounding them to bf16 would make the gradients' error half as
+// large again as the roundings of dg, du and the result make it; fp32 would double the traffic.  Kept are the upper 24
+// bits of the fp32 value (truncated: sign, exponent and 15 bits, an error below 2^-15), the upper 16 and the next 8 in
+// separate vectors.  The order is that of the accumulator tiles, where a thread holds 32 neighbouring columns of a row:
+// a block is 32 rows x 32 columns of g, then of u, each as 4 + 2 vectors of 16 bytes for every row, vector by vector, so
+// that a warp's stores and loads are whole 512-byte runs.
+constexpr int kGuHalf = 32 * 32 * 3;
+constexpr int kGuBlock = 2 * kGuHalf;
+__device__ __forceinline__ void gu_store(uint8_t* block, int lane, const uint32_t (&v)[32]) {
+  uint4* p = reinterpret_cast<uint4*>(block) + lane;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint4 h;
+    h.x = __byte_perm(v[8 * i + 0], v[8 * i + 1], 0x7632);
+    h.y = __byte_perm(v[8 * i + 2], v[8 * i + 3], 0x7632);
+    h.z = __byte_perm(v[8 * i + 4], v[8 * i + 5], 0x7632);
+    h.w = __byte_perm(v[8 * i + 6], v[8 * i + 7], 0x7632);
+    p[32 * i] = h;
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = 16 * i + 4 * j;
+      w[j] = __byte_perm(__byte_perm(v[c], v[c + 1], 0x0051), __byte_perm(v[c + 2], v[c + 3], 0x0051), 0x5410);
+    }
+    p[32 * (4 + i)] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+__device__ __forceinline__ void gu_fetch(const uint8_t* block, int lane, uint4 (&r)[6]) {
+  const uint4* p = reinterpret_cast<const uint4*>(block) + lane;
+#pragma unroll
+  for (int i = 0; i < 6; ++i) r[i] = p[32 * i];
+}
+// Column c (0..31) of a row's six vectors.
+__device__ __forceinline__ float gu_value(const uint4 (&r)[6], int c) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&r[0]);
+  const uint32_t hi = w[c >> 1], lo = w[16 + (c >> 2)];
+  // bytes of the value, low to high: 0, lo byte c & 3, the two of the upper half
+  const uint32_t h = (c & 1) ? __byte_perm(hi, 0u, 0x3244) : __byte_perm(hi, 0u, 0x1044);
+  return __uint_as_float(__byte_perm(h, lo, 0x3200 | ((4 + (c & 3)) << 4)));
+}
+// The same value by its place in the buffer, for the kernels whose threads do not hold rows of it.
+__device__ __forceinline__ size_t gu_block_offset(int row, int col, int col_blocks) {
+  return ((size_t)(row >> 5) * col_blocks + (col >> 5)) * kGuBlock;
+}
+__device__ __forceinline__ void gu_put(uint8_t* half, int r, int c, float v) {
+  const uint32_t b = __float_as_uint(v);
+  *reinterpret_cast<uint16_t*>(half + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2) = (uint16_t)(b >> 16);
+  half[((4 + (c >> 4)) * 32 + r) * 16 + (c & 15)] = (uint8_t)(b >> 8);
+}
+__device__ __forceinline__ float gu_get(const uint8_t* half, int r, int c) {
+  const uint32_t hi = *reinterpret_cast<const uint16_t*>(half + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2);
+  const uint32_t lo = half[((4 + (c >> 4)) * 32 + r) * 16 + (c & 15)];
+  return __uint_as_float((hi << 16) | (lo << 8));
+}
+
+}  // namespace
+}  // namespace asd
