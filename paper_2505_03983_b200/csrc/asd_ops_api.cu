@@ -103,7 +103,7 @@ asd_status run_matmul(const asd_ops* o, const asd_matmul_i8_args* a, Cut* cut, b
   g.b[0] = {aligned_operand(o, Mat{a->b, a->out, a->k, a->ld_b, 1}, cut, launch, st), false};
   g.c[0] = a->y, g.ldc = a->ld_y;
   g.scale_a = a->a_scale, g.scale_b = a->b_scale, g.bias = a->bias;
-  return launch ? ops_gemm(o, g, st) : ASD_OK;
+  return launch ? ops_gemm(o, g, false, st) : ASD_OK;
 }
 
 // ---- gated_mlp ----------------------------------------------------------------------------------------
@@ -134,13 +134,13 @@ asd_status run_forward(const asd_ops* o, const asd_gated_mlp_args* a, Cut* cut, 
   g.b[1] = {Mat{(const uint8_t*)w.p + 2 * w.ld * a->hidden, a->hidden, w.cols, w.ld, 2}, false};
   g.c[0] = h, g.ldc = hp;
   g.gu = a->saved ? (uint8_t*)a->saved + saved_h_bytes(a->rows, a->hidden) : nullptr;
-  CHECK(ops_gemm(o, g, st));
+  CHECK(ops_gemm(o, g, false, st));
   OpsGemm y{};
   y.epi = OPS_STORE, y.type = a->type, y.m = a->rows, y.n = a->width, y.k[0] = a->hidden, y.parts = y.groups = 1;
   y.a[0] = {Mat{h, a->rows, a->hidden, hp, 2}, false};
   y.b[0] = {wo, false};
   y.c[0] = a->y, y.ldc = a->ld_y;
-  return ops_gemm(o, y, st);
+  return ops_gemm(o, y, true, st);
 }
 
 asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, Cut* cut, bool launch, cudaStream_t st) {
@@ -161,7 +161,7 @@ asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, 
     g.b[0] = {wo, true};
     g.c[0] = dgu, g.c[1] = dgu + 2 * hp, g.ldc = 2 * hp;
     g.gu = (uint8_t*)a->saved + saved_h_bytes(rows, a->hidden);
-    CHECK(ops_gemm(o, g, st));
+    CHECK(ops_gemm(o, g, false, st));
   }
   if (a->dw_out) {  // dy^T h
     OpsGemm g{};
@@ -169,7 +169,7 @@ asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, 
     g.a[0] = {dy, true};
     g.b[0] = {Mat{a->saved, rows, a->hidden, hp, 2}, true};
     g.c[0] = a->dw_out, g.ldc = a->ld_dw_out;
-    CHECK(ops_gemm(o, g, st));
+    CHECK(ops_gemm(o, g, false, st));
   }
   if (a->dx) {  // dg Wg + du Wu
     OpsGemm g{};
@@ -178,7 +178,7 @@ asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, 
     g.b[0] = {Mat{w.p, a->hidden, w.cols, w.ld, 2}, true};
     g.b[1] = {Mat{(const uint8_t*)w.p + 2 * w.ld * a->hidden, a->hidden, w.cols, w.ld, 2}, true};
     g.c[0] = a->dx, g.ldc = a->ld_dx;
-    CHECK(ops_gemm(o, g, st));
+    CHECK(ops_gemm(o, g, false, st));
   }
   if (a->dw_in) {  // dg^T x and du^T x
     OpsGemm g{};
@@ -186,7 +186,7 @@ asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, 
     g.a[0] = {dg, true}, g.a[1] = {du, true};
     g.b[0] = g.b[1] = {x, true};
     g.c[0] = a->dw_in, g.c[1] = (uint8_t*)a->dw_in + 2 * a->ld_dw_in * a->hidden, g.ldc = a->ld_dw_in;
-    CHECK(ops_gemm(o, g, st));
+    CHECK(ops_gemm(o, g, false, st));
   }
   return ASD_OK;
 }

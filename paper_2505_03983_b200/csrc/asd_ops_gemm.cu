@@ -517,7 +517,8 @@ cudaError_t prepare_pair() {
 
 int64_t gated_saved_gu_bytes(int64_t rows, int64_t hidden) { return (rows + 31) / 32 * ((hidden + 31) / 32) * kGuBlock; }
 
-asd_status ops_gemm(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
+asd_status ops_gemm(const asd_ops* o, const OpsGemm& q, bool early, cudaStream_t st) {
+  if (use_stream(q)) return ops_gemm_stream(o, q, early, st);
   switch (q.epi) {
     case OPS_STORE: return launch_width<OPS_STORE>(o, q, st);
     case OPS_GATE: return launch_width<OPS_GATE>(o, q, st);

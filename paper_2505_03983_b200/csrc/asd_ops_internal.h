@@ -87,7 +87,13 @@ struct OpsGemm {
   const float* bias;
 };
 int64_t gated_saved_gu_bytes(int64_t rows, int64_t hidden);
-asd_status ops_gemm(const asd_ops* o, const OpsGemm& g, cudaStream_t st);
+// `early`: the kernel before this one in the stream belongs to the same call, which does not write b.
+asd_status ops_gemm(const asd_ops* o, const OpsGemm& g, bool early, cudaStream_t st);
 asd_status ops_gemm_prepare();  // per device: opt-in to large shared memory
+
+// ---- asd_ops_stream.cu: matrix products of few rows ---------------------------------------------------
+constexpr int kStreamMaxRows = 32;
+bool use_stream(const OpsGemm& g);
+asd_status ops_gemm_stream(const asd_ops* o, const OpsGemm& g, bool early, cudaStream_t st);
 
 }  // namespace asd

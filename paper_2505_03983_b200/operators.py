@@ -5,6 +5,7 @@ There is no CPU fallback: if the shared library has not been built, or no CUDA d
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional
 
 from .binding import AsdError, load_library
@@ -58,11 +59,19 @@ class _GatedMlpBackward(C.Structure):
                 ("workspace", _vp), ("workspace_bytes", _i64)]
 
 
+def _packer(cls):
+    """struct.pack of a structure's fields: the same bytes as the structure, in a fraction of its construction's time."""
+    return struct.Struct("@" + "".join({_i32: "i", _f32: "f", _i64: "q", _vp: "P"}[f[1]] for f in cls._fields_)).pack
+
+
+_pack_norm, _pack_norm_backward, _pack_quantize = _packer(_Norm), _packer(_NormBackward), _packer(_Quantize)
+_pack_matmul, _pack_mlp, _pack_mlp_backward = _packer(_MatmulI8), _packer(_GatedMlp), _packer(_GatedMlpBackward)
+
 _LIB = None
 
 
 def _library():
-    """The shared library with the operators' prototypes declared."""
+    """The shared library with the operators' prototypes declared.  Argument structures are passed as their bytes."""
     global _LIB
     if _LIB is None:
         lib = load_library()
@@ -70,28 +79,23 @@ def _library():
         lib.asd_ops_destroy.restype, lib.asd_ops_destroy.argtypes = None, [_vp]
         lib.asd_ops_create.argtypes = [C.POINTER(_vp)]
         lib.asd_ops_check.argtypes = [_vp, _vp]
-        for name, args in (("add_rmsnorm", _Norm), ("add_rmsnorm_backward", _NormBackward), ("quantize_i8", _Quantize),
-                           ("matmul_i8", _MatmulI8), ("gated_mlp_forward", _GatedMlp),
-                           ("gated_mlp_backward", _GatedMlpBackward)):
-            getattr(lib, "asd_" + name).argtypes = [_vp, C.POINTER(args), _vp]
-            if hasattr(lib, "asd_" + name + "_workspace"):
-                getattr(lib, "asd_" + name + "_workspace").argtypes = [_vp, C.POINTER(args), C.POINTER(_i64)]
-        lib.asd_gated_mlp_saved.argtypes = [_vp, C.POINTER(_GatedMlp), C.POINTER(_i64)]
         for name in OPS_SYMBOLS:
+            fn = getattr(lib, name)
             if name not in ("asd_ops_last_error", "asd_ops_destroy"):
-                getattr(lib, name).restype = C.c_int
+                fn.restype = C.c_int
+            if not name.startswith("asd_ops_"):
+                query = name.endswith(("_workspace", "_saved"))
+                fn.argtypes = [_vp, _vp, C.POINTER(_i64)] if query else [_vp, _vp, _vp]
         _LIB = lib
     return _LIB
 
 
-def _require(ok, message: str):
-    if not ok:
-        raise AsdError(1, message)
+def _fail(message: str):
+    raise AsdError(1, message)
 
 
 def _gate(act):
-    _require(act in ("silu", "gelu"), f'act must be "silu" or "gelu": {act!r}')
-    return ACT[act]
+    return ACT[act] if act == "silu" or act == "gelu" else _fail(f'act must be "silu" or "gelu": {act!r}')
 
 
 class AsdOps:
@@ -107,12 +111,16 @@ class AsdOps:
             raise AsdError(4, "no CUDA device: the ASD library has no CPU path")
         self._torch = torch
         self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # asd_type
+        self._i8, self._f32, self._u8 = torch.int8, torch.float32, torch.uint8
         self.lib = _library()
-        torch.cuda.init()
         self.device = torch.cuda.current_device()
-        torch.cuda.current_stream()  # the device's context exists before the library asks for it
-        self._handle = _vp()
-        self._check(self.lib.asd_ops_create(C.byref(self._handle)))
+        # the current stream's handle, by the shortest way that this torch has
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._stream = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        torch.cuda.current_stream().synchronize()  # the device's context exists before the library asks for it
+        handle = _vp()
+        self._check(self.lib.asd_ops_create(C.byref(handle)))
+        self._handle = handle.value
 
     # -- helpers -------------------------------------------------------------------------
     def _check(self, st: int):
@@ -137,75 +145,85 @@ class AsdOps:
             pass
 
     def _rows(self, t, name, width=None, dtype=None):
-        """(matrix of t's rows, distance of two rows)."""
-        _require(isinstance(t, self._torch.Tensor) and t.is_cuda and t.device.index == self.device,
-                 f"{name} must be a tensor on cuda:{self.device}")
-        _require(t.dim() >= 2, f"{name} must have two or more dimensions: it has {t.dim()}")
-        _require(width is None or t.shape[-1] == width, f"{name}: rows of {t.shape[-1]}, expected {width}")
-        _require(dtype is None or t.dtype == dtype, f"{name}: {t.dtype}, expected {dtype}")
-        _require(t.shape[-1] > 0, f"{name}: rows without elements")
+        """(t as a matrix of rows, its rows, their length, the distance of two)."""
+        if not isinstance(t, self._torch.Tensor) or t.get_device() != self.device:
+            _fail(f"{name} must be a tensor on cuda:{self.device}")
+        if dtype is not None and t.dtype is not dtype:
+            _fail(f"{name}: {t.dtype}, expected {dtype}")
         if t.dim() != 2:
+            if t.dim() < 2:
+                _fail(f"{name} must have two or more dimensions: it has {t.dim()}")
+            if t.shape[-1] == 0:
+                _fail(f"{name}: rows without elements")
             t = t.reshape(-1, t.shape[-1])
         n, w = t.shape
-        if w > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) < w:
-            t = t.contiguous()
-        return t, (t.stride(0) if n > 1 else w)
+        if width is not None and w != width:
+            _fail(f"{name}: rows of {w}, expected {width}")
+        if t.is_contiguous():
+            return (t, n, w, w) if w else _fail(f"{name}: rows without elements")
+        step, one = t.stride()
+        if w > 1 and one != 1 or n > 1 and step < w:
+            t, step = t.contiguous(), w
+        return t, n, w, step if n > 1 else w
 
-    def _vector(self, t, name, n, dtype=None):
-        _require(isinstance(t, self._torch.Tensor) and t.is_cuda and t.device.index == self.device,
-                 f"{name} must be a tensor on cuda:{self.device}")
-        _require(t.dim() == 1 and t.shape[0] == n, f"{name} must have the shape ({n},): {tuple(t.shape)}")
-        _require(dtype is None or t.dtype == dtype, f"{name}: {t.dtype}, expected {dtype}")
-        return t.contiguous()
+    def _vector(self, t, name, n, dtype):
+        if not isinstance(t, self._torch.Tensor) or t.get_device() != self.device:
+            _fail(f"{name} must be a tensor on cuda:{self.device}")
+        if t.dim() != 1 or t.shape[0] != n:
+            _fail(f"{name} must have the shape ({n},): {tuple(t.shape)}")
+        if dtype is not None and t.dtype is not dtype:
+            _fail(f"{name}: {t.dtype}, expected {dtype}")
+        return t if t.is_contiguous() else t.contiguous()
 
     def _type(self, t, name):
-        _require(t.dtype in self._types, f"{name}: unsupported type {t.dtype}")
-        return self._types[t.dtype]
+        kind = self._types.get(getattr(t, "dtype", None))
+        return _fail(f"{name} must be a tensor of float32, float16 or bfloat16") if kind is None else kind
 
-    def _new(self, shape, dtype):
-        return self._torch.empty(shape, dtype=dtype, device=self._torch.device("cuda", self.device))
+    def _weight(self, weight, w, kind):
+        """(w_type, weight, its address); without a weight that of the rows' type."""
+        if weight is None:
+            return kind, None, 0
+        weight = self._vector(weight, "weight", w, None)
+        return self._type(weight, "weight"), weight, weight.data_ptr()
 
-    def _call(self, name, args):
-        """asd_<name> on the current stream, with the workspace that it asks for."""
-        query = getattr(self.lib, "asd_" + name + "_workspace", None)
-        if query is not None:
-            need = _i64(0)
-            self._check(query(self._handle, C.byref(args), C.byref(need)))
-            if need.value:
-                space = self._new((need.value,), self._torch.uint8)
-                args.workspace, args.workspace_bytes = space.data_ptr(), need.value
-        self._check(getattr(self.lib, "asd_" + name)(self._handle, C.byref(args),
-                                                     self._torch.cuda.current_stream(self.device).cuda_stream))
+    def _space(self, query, args):
+        """The workspace that a call with these arguments asks for: (tensor or None, address, bytes)."""
+        need = _i64()
+        st = query(self._handle, args, need)
+        if st != 0:
+            self._check(st)
+        n = need.value
+        if not n:
+            return None, 0, 0
+        space = self._torch.empty(n, dtype=self._u8, device=self.device)
+        return space, space.data_ptr(), n
 
     def check(self):
         """Synchronises the current stream; raises ASD_ERR_TIMEOUT if a kernel of this handle gave up a wait."""
-        self._check(self.lib.asd_ops_check(self._handle, self._torch.cuda.current_stream(self.device).cuda_stream))
+        self._check(self.lib.asd_ops_check(self._handle, self._stream(self.device)))
 
     # -- norm ------------------------------------------------------------------------------
     def _norm(self, x, weight, residual, eps, q8):
-        torch = self._torch
         kind = self._type(x, "x")
-        shape, w = x.shape, x.shape[-1]
-        a = _Norm()
-        m, a.ld_x = self._rows(x, "x")
-        a.rows, a.width, a.type, a.eps, a.x = m.shape[0], w, kind, eps, m.data_ptr()
+        m, n, w, ld = self._rows(x, "x")
+        r_ptr = r_ld = s_ptr = s_ld = 0
+        total = x
         if residual is not None:
-            _require(residual.shape == shape, f"residual: {tuple(residual.shape)}, expected {tuple(shape)}")
-            r, a.ld_residual = self._rows(residual, "residual", dtype=x.dtype)
-            a.residual = r.data_ptr()
-        a.w_type = kind
-        if weight is not None:
-            weight = self._vector(weight, "weight", w)
-            a.w_type, a.weight = self._type(weight, "weight"), weight.data_ptr()
-        total = self._new(shape, x.dtype) if residual is not None else x
-        if residual is not None:
-            a.sum, a.ld_sum = total.data_ptr(), w
-        y = self._new(shape, torch.int8 if q8 else x.dtype)
-        a.y, a.ld_y = y.data_ptr(), w
-        scale = self._new(shape[:-1], torch.float32) if q8 else None
-        if q8 and a.rows:
-            a.scale = scale.data_ptr()
-        self._call("add_rmsnorm", a)
+            r, _, _, r_ld = self._rows(residual, "residual", w, x.dtype)
+            if residual.shape != x.shape:
+                _fail(f"residual: {tuple(residual.shape)}, expected {tuple(x.shape)}")
+            total = x.new_empty(x.shape)
+            r_ptr, s_ptr, s_ld = r.data_ptr(), total.data_ptr(), w
+        w_type, weight, w_ptr = self._weight(weight, w, kind)
+        if q8:
+            y, scale = x.new_empty(x.shape, dtype=self._i8), x.new_empty(x.shape[:-1], dtype=self._f32)
+            sc_ptr = scale.data_ptr()
+        else:
+            y, scale, sc_ptr = x.new_empty(x.shape), None, 0
+        st = self.lib.asd_add_rmsnorm(self._handle, _pack_norm(n, w, kind, w_type, eps, 0, m.data_ptr(), ld, r_ptr, r_ld, w_ptr, s_ptr, s_ld,
+                                                               y.data_ptr(), w, sc_ptr), self._stream(self.device))
+        if st != 0:
+            self._check(st)
         return y, scale, total
 
     def add_rmsnorm(self, x, weight, residual=None, eps=1e-6):
@@ -222,93 +240,105 @@ class AsdOps:
         """(dx, dweight) of add_rmsnorm from the gradients dy of y and ds of s (None: 0); dx is the gradient of x and of
         the residual alike, dweight has weight's type (s's without a weight), or is None if it is not needed."""
         kind = self._type(s, "s")
-        shape, w = s.shape, s.shape[-1]
-        a = _NormBackward()
-        _require(dy.shape == shape, f"dy: {tuple(dy.shape)}, expected {tuple(shape)}")
-        m, a.ld_s = self._rows(s, "s")
-        g, a.ld_dy = self._rows(dy, "dy", dtype=s.dtype)
-        a.rows, a.width, a.type, a.eps, a.s, a.dy = m.shape[0], w, kind, eps, m.data_ptr(), g.data_ptr()
+        m, n, w, ld = self._rows(s, "s")
+        g, _, _, g_ld = self._rows(dy, "dy", w, s.dtype)
+        d_ptr = d_ld = 0
         if ds is not None:
-            _require(ds.shape == shape, f"ds: {tuple(ds.shape)}, expected {tuple(shape)}")
-            d, a.ld_ds = self._rows(ds, "ds", dtype=s.dtype)
-            a.ds = d.data_ptr()
-        a.w_type = kind
-        if weight is not None:
-            weight = self._vector(weight, "weight", w)
-            a.w_type, a.weight = self._type(weight, "weight"), weight.data_ptr()
-        dx = self._new(shape, s.dtype)
-        a.dx, a.ld_dx = dx.data_ptr(), w
-        dw = None
+            d, _, _, d_ld = self._rows(ds, "ds", w, s.dtype)
+            d_ptr = d.data_ptr()
+        if dy.shape != s.shape or ds is not None and ds.shape != s.shape:
+            _fail(f"dy and ds must have the shape of s, {tuple(s.shape)}")
+        w_type, weight, w_ptr = self._weight(weight, w, kind)
+        dx = s.new_empty(s.shape)
+        dw, dw_ptr = None, 0
         if need_dweight:
-            dw = self._new((w,), s.dtype if weight is None else weight.dtype)
-            a.dw = dw.data_ptr()
-        self._call("add_rmsnorm_backward", a)
+            dw = s.new_empty(w, dtype=s.dtype if weight is None else weight.dtype)
+            dw_ptr = dw.data_ptr()
+        args = (n, w, kind, w_type, eps, 0, g.data_ptr(), g_ld, m.data_ptr(), ld, d_ptr, d_ld, w_ptr, dx.data_ptr(), w, dw_ptr)
+        space, at, size = self._space(self.lib.asd_add_rmsnorm_backward_workspace, _pack_norm_backward(*args, 0, 0))
+        st = self.lib.asd_add_rmsnorm_backward(self._handle, _pack_norm_backward(*args, at, size), self._stream(self.device))
+        if st != 0:
+            self._check(st)
         return dx, dw
 
     # -- 8 bits ----------------------------------------------------------------------------
     def quantize_i8(self, x, act: Optional[str] = None):
         """(q, scale) of the rows of x, or, with act "silu" or "gelu", of h = act(g) * u for rows [g | u]."""
-        _require(act in ACT, f'act must be None, "silu" or "gelu": {act!r}')
-        a = _Quantize()
-        a.type, a.act = self._type(x, "x"), ACT[act]
-        m, a.ld_x = self._rows(x, "x")
-        w = m.shape[1]
+        if act not in ACT:
+            _fail(f'act must be None, "silu" or "gelu": {act!r}')
+        kind = self._type(x, "x")
+        m, n, w, ld = self._rows(x, "x")
+        shape = x.shape
         if act is not None:
-            _require(w % 2 == 0, f"x: rows [g | u] of an even length, not {w}")
+            if w % 2:
+                _fail(f"x: rows [g | u] of an even length, not {w}")
             w //= 2
-        q = self._new(x.shape[:-1] + (w,), self._torch.int8)
-        scale = self._new(x.shape[:-1], self._torch.float32)
-        a.rows, a.width, a.x, a.q, a.ld_q, a.scale = m.shape[0], w, m.data_ptr(), q.data_ptr(), w, scale.data_ptr()
-        self._call("quantize_i8", a)
+            shape = shape[:-1] + (w,)
+        q, scale = x.new_empty(shape, dtype=self._i8), x.new_empty(shape[:-1], dtype=self._f32)
+        st = self.lib.asd_quantize_i8(self._handle, _pack_quantize(n, w, kind, ACT[act], m.data_ptr(), ld, q.data_ptr(), w, scale.data_ptr()),
+                                      self._stream(self.device))
+        if st != 0:
+            self._check(st)
         return q, scale
 
     def matmul_i8(self, a, a_scale, b, b_scale, bias=None, dtype=None):
         """(a b^T) * a_scale[..., None] * b_scale + bias in `dtype` (bfloat16): a [..., k] and b [out, k] int8, a_scale
         [...] a float32 per row (token), b_scale [out] one per row of b (channel), bias [out] float32 or None."""
-        torch = self._torch
-        dtype = torch.bfloat16 if dtype is None else dtype
-        _require(dtype in self._types, f"unsupported type {dtype}")
-        g = _MatmulI8()
-        ma, g.ld_a = self._rows(a, "a", dtype=torch.int8)
-        _require(b.dim() == 2, "b must be a matrix [out, k]")
-        mb, g.ld_b = self._rows(b, "b", width=ma.shape[1], dtype=torch.int8)
-        g.rows, g.out, g.k, g.out_type = ma.shape[0], mb.shape[0], ma.shape[1], self._types[dtype]
-        _require(a_scale.shape == a.shape[:-1], f"a_scale: {tuple(a_scale.shape)}, expected {tuple(a.shape[:-1])}")
-        sa = self._vector(a_scale.reshape(-1), "a_scale", g.rows, torch.float32)
-        sb = self._vector(b_scale, "b_scale", g.out, torch.float32)
-        g.a, g.b, g.a_scale, g.b_scale = ma.data_ptr(), mb.data_ptr(), sa.data_ptr(), sb.data_ptr()
+        dtype = self._torch.bfloat16 if dtype is None else dtype
+        if dtype not in self._types:
+            _fail(f"unsupported type {dtype}")
+        ma, n, k, ld_a = self._rows(a, "a", None, self._i8)
+        mb, out, _, ld_b = self._rows(b, "b", k, self._i8)
+        if b.dim() != 2:
+            _fail("b must be a matrix [out, k]")
+        shape = a.shape[:-1]
+        if a_scale.shape != shape:
+            _fail(f"a_scale: {tuple(a_scale.shape)}, expected {tuple(shape)}")
+        sa = self._vector(a_scale if a_scale.dim() == 1 else a_scale.reshape(-1), "a_scale", n, self._f32)
+        sb = self._vector(b_scale, "b_scale", out, self._f32)
+        bias_ptr = 0
         if bias is not None:
-            bias = self._vector(bias, "bias", g.out, torch.float32)
-            g.bias = bias.data_ptr()
-        y = self._new(a.shape[:-1] + (g.out,), dtype)
-        g.y, g.ld_y = y.data_ptr(), g.out
-        self._call("matmul_i8", g)
+            bias = self._vector(bias, "bias", out, self._f32)
+            bias_ptr = bias.data_ptr()
+        y = a.new_empty(shape + (out,), dtype=dtype)
+        args = (n, out, k, self._types[dtype], ma.data_ptr(), ld_a, mb.data_ptr(), ld_b, sa.data_ptr(), sb.data_ptr(), bias_ptr,
+                y.data_ptr(), out)
+        space, at, size = self._space(self.lib.asd_matmul_i8_workspace, _pack_matmul(*args, 0, 0))
+        st = self.lib.asd_matmul_i8(self._handle, _pack_matmul(*args, at, size), self._stream(self.device))
+        if st != 0:
+            self._check(st)
         return y
 
     # -- gated MLP ---------------------------------------------------------------------------
-    def _mlp_weights(self, a, dtype, w_in, w_out, width):
-        _require(w_in.dim() == 2 and w_in.shape[0] % 2 == 0, f"w_in must be a matrix [2 hidden, width]: {tuple(w_in.shape)}")
-        wi, a.ld_w_in = self._rows(w_in, "w_in", width=width, dtype=dtype)
-        _require(w_out.dim() == 2 and w_out.shape[0] == width, f"w_out must be a matrix [width, hidden]: {tuple(w_out.shape)}")
-        wo, a.ld_w_out = self._rows(w_out, "w_out", width=w_in.shape[0] // 2, dtype=dtype)
-        a.width, a.hidden, a.w_in, a.w_out = width, w_in.shape[0] // 2, wi.data_ptr(), wo.data_ptr()
-        return wi, wo
+    def _mlp_weights(self, dtype, w_in, w_out, width):
+        """(hidden, the two matrices, and their addresses with row distances)."""
+        wi, two, _, ld_i = self._rows(w_in, "w_in", width, dtype)
+        if w_in.dim() != 2 or two % 2 or two == 0:
+            _fail(f"w_in must be a matrix [2 hidden, width]: {tuple(w_in.shape)}")
+        wo, n, _, ld_o = self._rows(w_out, "w_out", two // 2, dtype)
+        if w_out.dim() != 2 or n != width:
+            _fail(f"w_out must be a matrix [width, hidden]: {tuple(w_out.shape)}")
+        return two // 2, (wi, wo), (wi.data_ptr(), ld_i, wo.data_ptr(), ld_o)
+
+    def _saved_bytes(self, n, w, hidden, kind, act):
+        need = _i64()
+        self._check(self.lib.asd_gated_mlp_saved(self._handle, _pack_mlp(n, w, hidden, kind, act, 0, *([0] * 11)), need))
+        return need.value
 
     def _mlp(self, x, w_in, w_out, act, keep):
-        a = _GatedMlp()
-        a.type, a.act = self._type(x, "x"), _gate(act)
-        m, a.ld_x = self._rows(x, "x")
-        a.rows, a.x = m.shape[0], m.data_ptr()
-        held = self._mlp_weights(a, x.dtype, w_in, w_out, m.shape[1])  # noqa: F841  (copies live until the call is enqueued)
-        y = self._new(x.shape, x.dtype)
-        a.y, a.ld_y = y.data_ptr(), m.shape[1]
-        saved = None
+        kind, act = self._type(x, "x"), _gate(act)
+        m, n, w, ld = self._rows(x, "x")
+        hidden, held, weights = self._mlp_weights(x.dtype, w_in, w_out, w)  # `held`: copies live until the call is enqueued
+        y = x.new_empty(x.shape)
+        saved, saved_ptr = None, 0
         if keep:
-            need = _i64(0)
-            self._check(self.lib.asd_gated_mlp_saved(self._handle, C.byref(a), C.byref(need)))
-            saved = self._new((need.value,), self._torch.uint8)
-            a.saved = saved.data_ptr() if need.value else None
-        self._call("gated_mlp_forward", a)
+            saved = x.new_empty(self._saved_bytes(n, w, hidden, kind, act), dtype=self._u8)
+            saved_ptr = saved.data_ptr()
+        args = (n, w, hidden, kind, act, 0, m.data_ptr(), ld, *weights, y.data_ptr(), w, saved_ptr)
+        space, at, size = self._space(self.lib.asd_gated_mlp_forward_workspace, _pack_mlp(*args, 0, 0))
+        st = self.lib.asd_gated_mlp_forward(self._handle, _pack_mlp(*args, at, size), self._stream(self.device))
+        if st != 0:
+            self._check(st)
         return y, saved
 
     def gated_mlp(self, x, w_in, w_out, act="silu"):
@@ -322,31 +352,24 @@ class AsdOps:
 
     def gated_mlp_backward(self, dy, x, w_in, w_out, saved, act="silu", need=(True, True, True)):
         """(dx, dw_in, dw_out); an entry of `need` that is false leaves out that gradient (None)."""
-        a = _GatedMlpBackward()
-        a.type, a.act = self._type(x, "x"), _gate(act)
-        _require(dy.shape == x.shape, f"dy: {tuple(dy.shape)}, expected {tuple(x.shape)}")
-        m, a.ld_x = self._rows(x, "x")
-        g, a.ld_dy = self._rows(dy, "dy", dtype=x.dtype)
-        a.rows, a.x, a.dy = m.shape[0], m.data_ptr(), g.data_ptr()
-        held = self._mlp_weights(a, x.dtype, w_in, w_out, m.shape[1])  # noqa: F841
-        f = _GatedMlp(rows=a.rows, width=a.width, hidden=a.hidden, type=a.type, act=a.act)
-        size = _i64(0)
-        self._check(self.lib.asd_gated_mlp_saved(self._handle, C.byref(f), C.byref(size)))
-        _require(saved.numel() == size.value and saved.dtype == self._torch.uint8 and saved.is_cuda and saved.is_contiguous(),
-                 f"saved must be what gated_mlp_forward returned: {size.value} bytes for these sizes")
-        if size.value:
-            a.saved = saved.data_ptr()
-        dx = dw_in = dw_out = None
-        if need[0]:
-            dx = self._new(x.shape, x.dtype)
-            a.dx, a.ld_dx = dx.data_ptr(), a.width
-        if need[1]:
-            dw_in = self._new(w_in.shape, x.dtype)
-            a.dw_in, a.ld_dw_in = dw_in.data_ptr(), a.width
-        if need[2]:
-            dw_out = self._new(w_out.shape, x.dtype)
-            a.dw_out, a.ld_dw_out = dw_out.data_ptr(), a.hidden
-        self._call("gated_mlp_backward", a)
+        kind, act = self._type(x, "x"), _gate(act)
+        m, n, w, ld = self._rows(x, "x")
+        g, _, _, g_ld = self._rows(dy, "dy", w, x.dtype)
+        if dy.shape != x.shape:
+            _fail(f"dy: {tuple(dy.shape)}, expected {tuple(x.shape)}")
+        hidden, held, weights = self._mlp_weights(x.dtype, w_in, w_out, w)
+        size = self._saved_bytes(n, w, hidden, kind, act)
+        if saved.dtype is not self._u8 or saved.numel() != size or saved.get_device() != self.device or not saved.is_contiguous():
+            _fail(f"saved must be what gated_mlp_forward returned: {size} bytes for these sizes")
+        dx = x.new_empty(x.shape) if need[0] else None
+        dw_in = x.new_empty(w_in.shape) if need[1] else None
+        dw_out = x.new_empty(w_out.shape) if need[2] else None
+        out = [0 if t is None else t.data_ptr() for t in (dx, dw_in, dw_out)]
+        args = (n, w, hidden, kind, act, 0, g.data_ptr(), g_ld, m.data_ptr(), ld, *weights, saved.data_ptr(), out[0], w, out[1], w, out[2], hidden)
+        space, at, size = self._space(self.lib.asd_gated_mlp_backward_workspace, _pack_mlp_backward(*args, 0, 0))
+        st = self.lib.asd_gated_mlp_backward(self._handle, _pack_mlp_backward(*args, at, size), self._stream(self.device))
+        if st != 0:
+            self._check(st)
         return dx, dw_in, dw_out
 
 
