@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libasd_b200.so")
 SOURCES = ["asd_api.cu", "asd_kernels.cu", "asd_resident.cu", "asd_gemm.cu", "asd_mlp_fused.cu", "asd_static.cu", "asd_schedule.cu",
-           "asd_ops_api.cu", "asd_ops_rows.cu", "asd_ops_gemm.cu", "asd_ops_stream.cu"]
+           "asd_ops_api.cu", "asd_ops_rows.cu", "asd_ops_gemm.cu", "asd_ops_stream.cu", "asd_ops_split.cu"]
 
 
 def _newest(paths):

@@ -282,6 +282,8 @@ asd_status asd_ops_create(asd_ops** out) {
     return ops_fail(ASD_ERR_CUDA, "cudaDeviceGetAttribute: %s", cudaGetErrorString(cudaGetLastError()));
   REQUIRE(major == 10, ASD_ERR_UNSUPPORTED, "the library is built for sm_100a; device %d has compute capability %d.x", dev, major);
   CHECK(ops_gemm_prepare());
+  CHECK(ops_stream_prepare());
+  CHECK(ops_split_prepare());
   asd_ops* o = new (std::nothrow) asd_ops();
   REQUIRE(o, ASD_ERR_OOM, "out of host memory");
   o->device = dev;

@@ -16,7 +16,7 @@
 //   GATE_GRAD  C = dh: dg = dh u act'(g), du = dh act(g)
 //   I8         C scale_a[m] scale_b[n] + bias[n], rounded to the output's type
 // An output whose address and row distance are multiples of 16 bytes leaves through shared memory by TMA stores of 128-byte
-// row pieces; the others are stored element by element.
+// row pieces; the others are staged in the same way and stored by lanes on neighbouring elements.
 #include <string.h>
 
 #include <algorithm>
@@ -95,20 +95,27 @@ __device__ __forceinline__ void stage_send(const CUtensorMap* map, uint32_t buf,
     bulk_commit();
   }
 }
-// 32 columns of a row element by element.
-__device__ __forceinline__ void store_row16(void* c, int64_t ldc, int row, int col, int m, int n, const uint32_t (&w)[16]) {
-  if (row >= m) return;
-  uint16_t* p = reinterpret_cast<uint16_t*>(c) + row * ldc + col;
+// The staged rows element by element, for outputs that the TMA cannot address: 32 lanes on 32 neighbouring columns.
+__device__ __forceinline__ void rows_out16(const uint8_t* buf, void* c, int64_t ldc, int lane, int row0, int col0, int m, int n) {
+  __syncwarp();
+  uint16_t* p = reinterpret_cast<uint16_t*>(c) + row0 * ldc + col0;
+  const int rows = min(32, m - row0);
+  for (int r = 0; r < rows; ++r, p += ldc) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (col + i < n) p[i] = (uint16_t)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1]);
+    for (int h = 0; h < 2; ++h) {
+      const int i = 32 * h + lane;
+      if (col0 + i < n) p[i] = *reinterpret_cast<const uint16_t*>(buf + r * 128 + (((i >> 3) ^ (r & 7)) << 4) + 2 * (i & 7));
+    }
+  }
+  __syncwarp();
 }
-__device__ __forceinline__ void store_row32(void* c, int64_t ldc, int row, int col, int m, int n, const float (&f)[32]) {
-  if (row >= m) return;
-  float* p = reinterpret_cast<float*>(c) + row * ldc + col;
-#pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (col + i < n) p[i] = f[i];
+__device__ __forceinline__ void rows_out32(const uint8_t* buf, void* c, int64_t ldc, int lane, int row0, int col0, int m, int n) {
+  __syncwarp();
+  uint32_t* p = reinterpret_cast<uint32_t*>(c) + row0 * ldc + col0;
+  const int rows = min(32, m - row0);
+  for (int r = 0; r < rows; ++r, p += ldc)
+    if (col0 + lane < n) p[lane] = *reinterpret_cast<const uint32_t*>(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + 4 * (lane & 3));
+  __syncwarp();
 }
 __device__ __forceinline__ void stage_half(uint8_t* buf, int lane, int half, const uint32_t (&w)[16]) {
 #pragma unroll
@@ -328,12 +335,12 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
                   w[i] = pack16(h0, h1, f16);
                 }
               }
-              if (g.tma_store)
-                stage_half(buf, lane, h, w);
-              else
-                store_row16(g.c[tile.group], g.ldc, row, col, g.m, g.n, w);
+              stage_half(buf, lane, h, w);
             }
-            if (g.tma_store) stage_send(&maps.c[tile.group], buf_addr, lane, col0, row0, any);
+            if (g.tma_store)
+              stage_send(&maps.c[tile.group], buf_addr, lane, col0, row0, any);
+            else
+              rows_out16(buf, g.c[tile.group], g.ldc, lane, row0, col0, g.m, g.n);
           } else if (EPI == OPS_GATE_GRAD) {
             stage_free(lane);
 #pragma unroll
@@ -384,27 +391,28 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
               for (int i = 0; i < 32; ++i)
                 f[i] = fmaf((float)(int)r[i] * sa, __shfl_sync(0xffffffffu, sb, i), __shfl_sync(0xffffffffu, bb, i));
               if (f32) {
-                if (g.tma_store) {
-                  if (h == 1) stage_free(lane);
+                if (g.tma_store && h == 1) stage_free(lane);
 #pragma unroll
-                  for (int i = 0; i < 8; ++i)
-                    stage_put(buf, lane, i, make_uint4(__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]),
-                                                       __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3])));
+                for (int i = 0; i < 8; ++i)
+                  stage_put(buf, lane, i, make_uint4(__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]),
+                                                     __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3])));
+                if (g.tma_store)
                   stage_send(&maps.c[0], buf_addr, lane, col, row0, rows_any && col < g.n);
-                } else {
-                  store_row32(g.c[0], g.ldc, row, col, g.m, g.n, f);
-                }
+                else
+                  rows_out32(buf, g.c[0], g.ldc, lane, row0, col, g.m, g.n);
               } else {
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = pack16(f[2 * i], f[2 * i + 1], f16);
-                if (g.tma_store)
-                  stage_half(buf, lane, h, w);
-                else
-                  store_row16(g.c[0], g.ldc, row, col, g.m, g.n, w);
+                stage_half(buf, lane, h, w);
               }
             }
-            if (g.tma_store && !f32) stage_send(&maps.c[0], buf_addr, lane, col0, row0, any);
+            if (!f32) {
+              if (g.tma_store)
+                stage_send(&maps.c[0], buf_addr, lane, col0, row0, any);
+              else
+                rows_out16(buf, g.c[0], g.ldc, lane, row0, col0, g.m, g.n);
+            }
           }
         }
       }
@@ -443,10 +451,14 @@ bool encode(CUtensorMap* out, CUtensorMapDataType dt, int es, const void* p, int
   return fn(out, dt, 2, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+}  // namespace
+
 bool encode_operand(CUtensorMap* out, const Operand& x, int type, bool i8, int tile_rows) {
   const CUtensorMapDataType dt = i8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : map_type(type);
   return encode(out, dt, x.mat.es, x.mat.p, x.mat.rows, x.mat.cols, x.mat.ld, x.mn ? 64 : tile_rows);
 }
+
+namespace {
 
 template <int BN, int EPI>
 asd_status launch_pair(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
@@ -495,17 +507,19 @@ asd_status launch_pair(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
   return ops_launched("matrix product");
 }
 
-// Tile width: the one whose waves of tiles take less time; a tile costs the larger of its MMAs' time and its operands'
-// way into shared memory (a k-block of 128 bytes: 2 BN clocks, 128 (128 + BN / 2) bytes at some 50 bytes a clock).
+// Clocks of a launch with tiles of width bn: waves of tiles, of which one costs the larger of its MMAs' time and its
+// operands' way into shared memory (a k-block of 128 bytes: 2 bn clocks, 128 (128 + bn / 2) bytes at some 50 bytes a
+// clock); some 5000 to start, drain the last tile and end.
+double pair_clocks(const asd_ops* o, const OpsGemm& q, int bn) {
+  const int cn = q.epi == OPS_GATE ? bn / 2 : bn, ke = q.epi == OPS_I8 ? 128 : 64;
+  const int64_t kb = (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
+  const int64_t tiles = (int64_t)q.groups * ((q.m + 2 * BM - 1) / (2 * BM)) * ((q.n + cn - 1) / cn);
+  const int64_t waves = (tiles + o->num_sms / 2 - 1) / (o->num_sms / 2);
+  return (double)(waves * kb) * std::max(2.0 * bn, (BM + bn / 2) * 128 / 50.0) + 5000.0;
+}
 template <int EPI>
 asd_status launch_width(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
-  auto cost = [&](int bn) {
-    const int cn = EPI == OPS_GATE ? bn / 2 : bn;
-    const int64_t tiles = (int64_t)q.groups * ((q.m + 2 * BM - 1) / (2 * BM)) * ((q.n + cn - 1) / cn);
-    const int64_t waves = (tiles + o->num_sms / 2 - 1) / (o->num_sms / 2);
-    return (double)waves * std::max(2.0 * bn, (BM + bn / 2) * 128 / 50.0);
-  };
-  return cost(256) <= cost(128) ? launch_pair<256, EPI>(o, q, st) : launch_pair<128, EPI>(o, q, st);
+  return pair_clocks(o, q, 256) <= pair_clocks(o, q, 128) ? launch_pair<256, EPI>(o, q, st) : launch_pair<128, EPI>(o, q, st);
 }
 
 template <int BN, int EPI>
@@ -519,6 +533,10 @@ int64_t gated_saved_gu_bytes(int64_t rows, int64_t hidden) { return (rows + 31) 
 
 asd_status ops_gemm(const asd_ops* o, const OpsGemm& q, bool early, cudaStream_t st) {
   if (use_stream(q)) return ops_gemm_stream(o, q, early, st);
+  if (q.groups == 1 && !q.a[0].mn) {
+    const SplitPlan p = plan_split(o, q);
+    if (p.clocks < std::min(pair_clocks(o, q, 256), pair_clocks(o, q, 128))) return ops_gemm_split(o, q, p, early, st);
+  }
   switch (q.epi) {
     case OPS_STORE: return launch_width<OPS_STORE>(o, q, st);
     case OPS_GATE: return launch_width<OPS_GATE>(o, q, st);

@@ -92,8 +92,21 @@ asd_status ops_gemm(const asd_ops* o, const OpsGemm& g, bool early, cudaStream_t
 asd_status ops_gemm_prepare();  // per device: opt-in to large shared memory
 
 // ---- asd_ops_stream.cu: matrix products of few rows ---------------------------------------------------
-constexpr int kStreamMaxRows = 32;
+constexpr int kStreamMaxRows = 8;
+asd_status ops_stream_prepare();
 bool use_stream(const OpsGemm& g);
 asd_status ops_gemm_stream(const asd_ops* o, const OpsGemm& g, bool early, cudaStream_t st);
+
+// ---- asd_ops_split.cu: matrix products with too few tiles ----------------------------------------------
+struct SplitPlan {
+  int nb, split, stages;  // rows of a CTA, CTAs that share a sum, stages of its operands
+  double clocks;          // estimate
+};
+SplitPlan plan_split(const asd_ops* o, const OpsGemm& g);
+asd_status ops_split_prepare();
+asd_status ops_gemm_split(const asd_ops* o, const OpsGemm& g, const SplitPlan& p, bool early, cudaStream_t st);
+
+// A tensor map of an operand: boxes of 128 bytes by `tile_rows` rows, or of 64 by 64 elements where it is read across k.
+bool encode_operand(CUtensorMap* out, const Operand& x, int type, bool i8, int tile_rows);
 
 }  // namespace asd

@@ -1,0 +1,357 @@
+// Matrix products with too few tiles to fill the SMs: C[m, n] = sum_k A(m, k) B(n, k) for some tens to hundreds of rows.
+//
+// A CTA owns 128 columns of C (GATE: 64, with the gate's and the value's weights for them) and up to 256 rows, and a
+// cluster of 1 to 8 CTAs shares the sum over k.  The operands change places: the weights are the 128-row operand of
+// tcgen05.mma and the rows of A the narrow one, so that few rows cost no padded tensor work and the 32 lanes of a warp
+// store 32 neighbouring columns of a row of C.  Each CTA parks its partial sums in its own shared memory as
+// [row of C][column]; after one cluster barrier every CTA adds up its share of the rows over distributed shared memory in
+// the order of the ranks (the same bits in every run), applies the epilogue and stores.
+#include <string.h>
+
+#include <algorithm>
+
+#include "asd_ops_tc.cuh"
+
+namespace asd {
+namespace {
+
+constexpr int kSplitThreads = 64 + 256;  // a TMA warp, an MMA warp, eight epilogue warps
+constexpr int kMostStages = 8;
+
+struct SplitMaps {
+  CUtensorMap w[2], x[2];
+};
+struct SplitArgs {
+  int m, n;
+  int kb[2];   // k-blocks of the first and of the second sum
+  int nb;      // rows of C to a CTA: a multiple of 16
+  int split;   // CTAs of a cluster
+  int stages;
+  int w_mn;    // the weights are read across k
+  int early;   // the weights may be read before the previous kernel has ended
+  uint32_t idesc, tmem_cols;
+  int out_type, gelu;
+  void* c[2];
+  int64_t ldc;
+  uint8_t* gu;
+  int gu_cols;
+  const float* scale_a;
+  const float* scale_b;
+  const float* bias;
+  int* err;
+};
+
+__host__ __device__ constexpr int split_stage_bytes(int nb) { return (BM + nb) * 128; }
+
+template <int EPI>
+__global__ void __launch_bounds__(kSplitThreads, 1)
+split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ SplitArgs g) {
+  constexpr bool I8 = EPI == OPS_I8;
+  constexpr int F = EPI == OPS_GATE ? 64 : 128;  // columns of C to a CTA
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t tiles = (raw + 1023u) & ~1023u;
+  const int stage_bytes = split_stage_bytes(g.nb);
+  uint8_t* tiles_ptr = smem_raw + (tiles - raw);
+  const int S = g.stages;
+  uint8_t* aux = tiles_ptr + max(S * stage_bytes, g.nb * BM * 4);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(aux);  // full[S], empty[S], acc_full
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aux + 8 * (2 * S + 1));
+  volatile int* dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const uint32_t bar0 = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };
+  const uint32_t accf_bar = bar0 + 8u * (2 * S);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank();
+  const int n0 = ((int)blockIdx.x / g.split) * F;
+  const int row0 = (int)blockIdx.y * g.nb;
+  const int num_kb = g.kb[0] + g.kb[1];
+  const int per = (num_kb + g.split - 1) / g.split;  // k-blocks [kb0, kb1) belong to this rank
+  const int kb0 = min(rank * per, num_kb), kb1 = min(kb0 + per, num_kb);
+  const uint32_t tmem_cols = g.tmem_cols;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      prefetch_tmap(&maps.w[i]);
+      prefetch_tmap(&maps.x[i]);
+    }
+    for (int s = 0; s < S; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(accf_bar, 1);
+    *dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(tmem_cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  if (!g.early) grid_dependency_wait();
+
+  if (warp == 0) {
+    // ---------------- TMA producer ----------------
+    if (lane == 0) {
+      auto load_w = [&](int stage, int kb) {
+        const int part = kb >= g.kb[0] ? 1 : 0;
+        const int k0 = (kb - part * g.kb[0]) * (I8 ? 128 : 64);
+        const uint32_t sw = tiles + stage * stage_bytes;
+        mbar_expect_tx(full_bar(stage), (uint32_t)stage_bytes);
+        if (EPI == OPS_GATE) {
+          tma_load_2d(sw, &maps.w[0], full_bar(stage), k0, n0);
+          tma_load_2d(sw + 64 * 128, &maps.w[1], full_bar(stage), k0, n0);
+        } else if (!g.w_mn) {
+          tma_load_2d(sw, &maps.w[part], full_bar(stage), k0, n0);
+        } else {
+          tma_load_2d(sw, &maps.w[part], full_bar(stage), n0, k0);
+          tma_load_2d(sw + 8192, &maps.w[part], full_bar(stage), n0 + 64, k0);
+        }
+      };
+      auto load_x = [&](int stage, int kb) {
+        const int part = kb >= g.kb[0] ? 1 : 0;
+        tma_load_2d(tiles + stage * stage_bytes + BM * 128, &maps.x[part], full_bar(stage), (kb - part * g.kb[0]) * (I8 ? 128 : 64), row0);
+      };
+      // the first stages are free: weights now, rows of A once the kernel that makes them has ended
+      const int pre = min(S, kb1 - kb0);
+      for (int i = 0; i < pre; ++i) load_w(i, kb0 + i);
+      if (g.early) grid_dependency_wait();
+      for (int i = 0; i < pre; ++i) load_x(i, kb0 + i);
+      int stage = pre == S ? 0 : pre;
+      uint32_t phase = pre == S ? 1u : 0u;
+      for (int kb = kb0 + pre; kb < kb1; ++kb) {
+        mbar_wait(empty_bar(stage), phase ^ 1u, dead, g.err);
+        load_w(stage, kb);
+        load_x(stage, kb);
+        if (++stage == S) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+      drain_after_timeout(dead);
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer ----------------
+    if (lane == 0) {
+      const uint64_t step_w = desc_step(g.w_mn);
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        mbar_wait(full_bar(stage), phase, dead, g.err);
+        tc_fence_after();
+        const uint32_t sw = tiles + stage * stage_bytes;
+        const uint64_t da = smem_desc(sw, g.w_mn), db = smem_desc(sw + BM * 128, false);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          tc_mma<I8, 1>(tmem_base, da + step_w * k, db + (uint64_t)(2 * k), g.idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+        tc_commit(empty_bar(stage));
+        if (++stage == S) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+      if (kb1 > kb0)
+        tc_commit(accf_bar);
+      else
+        mbar_arrive(accf_bar);  // no k-block of its own: the partial is zero
+    }
+  } else {
+    // ---- park this rank's partial sums as part[row][column] ----
+    const int quarter = warp & 3, half = (warp - kEpiWarp0) >> 2;  // the two warps of a lane quarter take alternate groups of 16 rows
+    const int feat = quarter * 32 + lane;
+    mbar_wait(accf_bar, 0u, dead, g.err);
+    tc_fence_after();
+    uint32_t* part = reinterpret_cast<uint32_t*>(tiles_ptr);  // the stages are idle now
+    for (int c0 = half * 16; c0 < g.nb; c0 += 32) {
+      uint32_t r[16];
+      if (kb1 > kb0) {
+        tc_ld16(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0, r);
+        tc_wait_ld();
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) r[e] = 0u;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) part[(c0 + e) * BM + feat] = r[e];
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  __syncwarp();
+  cluster_sync_all();  // every rank's partial sums are in place
+  grid_launch_dependents();
+
+  if (warp >= kEpiWarp0) {
+    if (g.early) grid_dependency_wait();  // what is stored below may still be in use by an earlier kernel
+    const int tid = (int)threadIdx.x - 64;
+    const int f = tid % F, col = n0 + f;
+    constexpr int kRows = 256 / F;  // rows of C that the eight warps work on side by side
+    const int m = min(g.m - row0, g.nb);
+    const bool f16 = g.out_type == ASD_TYPE_F16, gelu = g.gelu != 0;
+    if (col < g.n) {
+      float sb = 0.f, bb = 0.f;
+      if (I8) {
+        sb = g.scale_b[col];
+        bb = g.bias ? g.bias[col] : 0.f;
+      }
+      constexpr int R = 4;  // rows whose loads are in flight together
+      for (int lr0 = rank + (tid / F) * g.split; lr0 < m; lr0 += R * kRows * g.split) {
+        uint32_t v[R], u[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = u[i] = 0u;
+        for (int q = 0; q < g.split; ++q) {
+          const uint32_t base = map_to_cta(tiles, (uint32_t)q) + (uint32_t)(4 * f);
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const int lr = min(lr0 + i * kRows * g.split, m - 1);  // rows beyond the last are added up and not stored
+            const uint32_t p = __float_as_uint(ld_cluster_f32(base + (uint32_t)(lr * BM * 4)));
+            v[i] = I8 ? v[i] + p : __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(p));
+            if (EPI == OPS_GATE)
+              u[i] = __float_as_uint(__uint_as_float(u[i]) + ld_cluster_f32(base + (uint32_t)(lr * BM * 4 + 256)));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const int row = row0 + lr0 + i * kRows * g.split;
+          if (row >= row0 + m) break;
+          const float y = __uint_as_float(v[i]);
+          const int64_t at = row * g.ldc + col;
+          if (EPI == OPS_STORE) {
+            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(y, f16);
+          } else if (EPI == OPS_GATE) {
+            const float w = __uint_as_float(u[i]);
+            if (g.gu) {
+              uint8_t* b = g.gu + gu_block_offset(row, col, g.gu_cols);
+              gu_put(b, row & 31, col & 31, y);
+              gu_put(b + kGuHalf, row & 31, col & 31, w);
+            }
+            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(gate_value(y, gelu) * w, f16);
+          } else if (EPI == OPS_GATE_GRAD) {
+            const uint8_t* b = g.gu + gu_block_offset(row, col, g.gu_cols);
+            float a, da;
+            gate_grad(gu_get(b, row & 31, col & 31), gelu, a, da);
+            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(y * gu_get(b + kGuHalf, row & 31, col & 31) * da, f16);
+            reinterpret_cast<uint16_t*>(g.c[1])[at] = round16(y * a, f16);
+          } else {
+            const float z = fmaf((float)(int)v[i] * g.scale_a[row], sb, bb);
+            if (g.out_type == ASD_TYPE_F32)
+              reinterpret_cast<float*>(g.c[0])[at] = z;
+            else
+              reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(z, f16);
+          }
+        }
+      }
+    }
+  }
+
+  // no CTA leaves while a peer may still read its partial sums
+  tc_fence_before();
+  __syncthreads();
+  __syncwarp();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(tmem_cols) : "memory");
+  }
+}
+
+uint32_t split_tmem_cols(int nb) { return nb <= 32 ? 32u : (nb <= 64 ? 64u : (nb <= 128 ? 128u : 256u)); }
+// Shared memory of a CTA: at least as large a share of the SM's 228 KB as it takes of the 512 tensor-memory columns (452
+// bytes a column next to the 1 KB that every block costs).  CTAs that fit an SM together then never wait for one another's
+// tensor memory, which the members of a cluster, who wait for one another anyway, must not do.
+int split_smem(int nb, int stages) {
+  return std::max({stages * split_stage_bytes(nb) + 1280, nb * BM * 4 + 1280, (int)split_tmem_cols(nb) * 452});
+}
+
+template <int EPI>
+asd_status launch_split(const asd_ops* o, const OpsGemm& q, const SplitPlan& p, bool early, cudaStream_t st) {
+  constexpr bool I8 = EPI == OPS_I8;
+  constexpr int F = EPI == OPS_GATE ? 64 : 128;
+  SplitMaps maps;
+  memset(&maps, 0, sizeof(maps));
+  SplitArgs g{};
+  const int ke = I8 ? 128 : 64;
+  g.m = (int)q.m, g.n = (int)q.n;
+  g.kb[0] = (int)((q.k[0] + ke - 1) / ke);
+  g.kb[1] = q.parts == 2 ? (int)((q.k[1] + ke - 1) / ke) : 0;
+  g.nb = p.nb, g.split = p.split, g.stages = p.stages;
+  g.tmem_cols = split_tmem_cols(p.nb);
+  g.w_mn = q.b[0].mn;
+  g.early = early;
+  const uint32_t fmt = I8 ? 1u : (q.type == ASD_TYPE_BF16 ? 1u : 0u);
+  g.idesc = (I8 ? 2u << 4 : 1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)g.w_mn << 15) | ((uint32_t)(p.nb >> 3) << 17) |
+            ((uint32_t)(BM >> 4) << 24);
+  g.out_type = q.type, g.gelu = q.act == ASD_ACT_GELU;
+  g.c[0] = q.c[0], g.c[1] = q.c[1], g.ldc = q.ldc;
+  g.gu = q.gu, g.gu_cols = (int)((q.n + 31) / 32);
+  g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias;
+  g.err = o->err;
+  bool ok = true;
+  for (int i = 0; i < 2; ++i) {
+    ok = ok && encode_operand(&maps.w[i], q.b[EPI == OPS_GATE || q.parts == 2 ? i : 0], q.type, I8, F);
+    ok = ok && encode_operand(&maps.x[i], q.a[q.parts == 2 ? i : 0], q.type, I8, p.nb);
+  }
+  if (!ok) return ops_fail(ASD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+  const dim3 grid((unsigned)((q.n + F - 1) / F * p.split), (unsigned)((q.m + p.nb - 1) / p.nb));
+  ops_launch(split_kernel<EPI>, grid, dim3(kSplitThreads), (size_t)split_smem(p.nb, p.stages), st, p.split, maps, g);
+  return ops_launched("split matrix product");
+}
+
+template <int EPI>
+cudaError_t prepare_split() {
+  return cudaFuncSetAttribute(split_kernel<EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
+}
+
+}  // namespace
+
+// The cheapest way to split.  Clocks of a CTA: its k-blocks at the larger of the MMAs' time (nb / 128 of 256 clocks) and
+// its share of the SM's way into shared memory (some 50 bytes a clock), then some 3000 to join the partial sums and start
+// and end, and 8 for each row that a CTA adds up.
+SplitPlan plan_split(const asd_ops* o, const OpsGemm& q) {
+  const int ke = q.epi == OPS_I8 ? 128 : 64, F = q.epi == OPS_GATE ? 64 : 128;
+  const int64_t kb = (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
+  const int64_t tiles_n = (q.n + F - 1) / F;
+  SplitPlan best{16, 1, 2, 1e300};
+  for (int blocks = (int)((q.m + 255) / 256); blocks <= (int)((q.m + 255) / 256) + 8; ++blocks) {
+    const int nb = (int)std::max<int64_t>(16, ((q.m + blocks - 1) / blocks + 15) / 16 * 16);
+    if (nb > 256) continue;
+    const int64_t tiles_m = (q.m + nb - 1) / nb;
+    for (int split = 1; split <= 8; split *= 2) {
+      if (split > 1 && kb / split < 2) break;
+      const int64_t ctas = tiles_n * tiles_m * split;
+      // two CTAs to an SM where their shared memory allows it and there are enough of them
+      const int two = nb <= 128 && ctas > o->num_sms ? 2 : 1;
+      const int64_t waves = (ctas + two * o->num_sms - 1) / (two * o->num_sms);
+      const double fill = two * (BM + nb) * 128 / 50.0, math = two * std::max(128.0, 2.0 * nb);
+      const double t = waves * ((double)((kb + split - 1) / split) * std::max(fill, math) + 3000.0 + 8.0 * nb / split * split);
+      if (t < best.clocks) {
+        const int budget = two == 2 ? 110 * 1024 : 220 * 1024;
+        const int stages = std::max(2, std::min({kMostStages, budget / split_stage_bytes(nb), (int)std::max<int64_t>(2, (kb + split - 1) / split)}));
+        best = SplitPlan{nb, split, stages, t};
+      }
+    }
+  }
+  return best;
+}
+
+asd_status ops_gemm_split(const asd_ops* o, const OpsGemm& q, const SplitPlan& p, bool early, cudaStream_t st) {
+  switch (q.epi) {
+    case OPS_STORE: return launch_split<OPS_STORE>(o, q, p, early, st);
+    case OPS_GATE: return launch_split<OPS_GATE>(o, q, p, early, st);
+    case OPS_GATE_GRAD: return launch_split<OPS_GATE_GRAD>(o, q, p, early, st);
+    default: return launch_split<OPS_I8>(o, q, p, early, st);
+  }
+}
+
+asd_status ops_split_prepare() {
+  for (cudaError_t e : {prepare_split<OPS_STORE>(), prepare_split<OPS_GATE>(), prepare_split<OPS_GATE_GRAD>(), prepare_split<OPS_I8>()})
+    if (e != cudaSuccess) return ops_fail(ASD_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+  return ASD_OK;
+}
+
+}  // namespace asd

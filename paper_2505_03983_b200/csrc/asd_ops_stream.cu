@@ -1,12 +1,13 @@
-// Matrix products of few rows: y[i, j] = sum_k x[i, k] w[j, k] for up to 32 rows i.
+// Matrix products of few rows: y[i, j] = sum_k x[i, k] w[j, k] for up to 8 rows i.
 //
-// The time is that of reading w once, so the weights go from memory straight into the registers of the warps that multiply
-// them, without shared memory, barriers or tensor memory in between.  A warp owns 16 rows of w (GATE: 8 of the gate and the
-// same 8 of the value) and a share of k; they are the 16-row operand of mma.sync, the rows of x the narrow one.  The order
-// of k inside a sum is free as long as both operands have the same, so a lane takes 16 consecutive bytes of a row of w and
-// of a row of x and feeds them to two MMAs as they are: lane (g, t) holds rows g and g + 8 of w and row g of x, bytes
-// 16 t ... of each 64.  Each warp keeps 8 to 16 such loads in flight.  The eight warps of a block share 16 to 128 rows of w
-// and split k between them; their partial sums meet in shared memory in a fixed order.
+// The time is that of reading w once.  The 16 warps of a block work on 16 rows of w at a time (GATE: 8 of the gate and the
+// same 8 of the value) and share k; x stays in shared memory.  The rows of w are the 16-row operand of mma.sync, those of x
+// the narrow one.  The order of k inside a sum is free as long as both operands have the same, so a lane takes 16
+// consecutive bytes of a row of w and of a row of x and feeds them to two MMAs as they are: lane (g, t) holds rows g and
+// g + 8 of w and row g of x, bytes 16 t ... of each 64.  Every lane therefore reads back only what it has copied itself: the
+// weights come through a ring in shared memory of its own (cp.async, up to 11 steps of 1 KB a warp ahead, 176 KB an SM),
+// which needs neither barriers nor registers, and runs on over the block's next rows while the sums of one group of rows
+// meet (in shared memory, in a fixed order).
 #include <algorithm>
 
 #include "asd_ops_tc.cuh"
@@ -14,14 +15,16 @@
 namespace asd {
 namespace {
 
-constexpr int kStreamWarps = 8;
-constexpr int kStreamUnroll = 4;  // loads of a row of w that are issued together
+constexpr int kStreamWarps = 16;
+
+constexpr int kStreamSmem = 232448 - 2 * kStreamWarps * 8 * 17 * 4;  // of a block, without the partial sums
+constexpr int ring_bytes(int ring) { return kStreamWarps * ring * 1024; }
 
 struct StreamArgs {
   const uint8_t *w0, *w1, *x;  // GATE: w0 the gate's rows, w1 the value's; otherwise w1 = w0
   int64_t ld_w, ld_x;          // bytes
   int rows, n, k_bytes;        // rows of x, rows of w, bytes of a row's elements
-  int split;                   // warps that share a k: 1, 2, 4, 8
+  int pitch;                   // bytes from one row of x to the next in shared memory
   int early;                   // w may be read before the previous kernel has ended
   int out_type, gelu;
   void* c;
@@ -33,11 +36,9 @@ struct StreamArgs {
   const float* bias;
 };
 
-// Weights are read once: past L1, which is left to x.
-__device__ __forceinline__ uint4 load_once(const uint8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.L2::128B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+// 16 bytes to shared memory, of which `bytes` are read and the others zero.
+__device__ __forceinline__ void copy_16(uint32_t dst, const uint8_t* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 // The last bytes of a row: what lies beyond it counts as zero.
 __device__ __forceinline__ uint4 load_part(const uint8_t* p, int bytes) {
@@ -71,96 +72,89 @@ __device__ __forceinline__ void mma_16x8(uint32_t (&c)[4], uint32_t a0, uint32_t
   }
 }
 
-// NT: groups of 8 rows of x.
-template <int KIND, int NT, int EPI>
-__global__ void __launch_bounds__(32 * kStreamWarps, 2) stream_kernel(const StreamArgs a) {
-  constexpr int FR = EPI == OPS_GATE ? 8 : 16;  // rows of w, or columns of h, of a warp
-  constexpr int U = kStreamUnroll;
-  __shared__ uint32_t part[kStreamWarps][NT * 8][17];  // a warp's sums: [row of x][row of w]
+// RING: steps of the ring.
+template <int KIND, int EPI, int RING>
+__global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const StreamArgs a) {
+  constexpr int FR = EPI == OPS_GATE ? 8 : 16;  // columns of the output to a group of rows of w
+  extern __shared__ __align__(128) uint8_t smem[];  // the warps' rings, then x
+  __shared__ uint32_t part[2][kStreamWarps][8][17];  // a warp's sums: [row of x][row of w]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int groups = kStreamWarps / a.split;  // of FR rows, in this block
-  const int f0 = (blockIdx.x * groups + warp / a.split) * FR;
-  const int share = warp % a.split;
-  const uint8_t* p0 = a.w0 + (int64_t)min(f0 + g, a.n - 1) * a.ld_w + 16 * t;
-  const uint8_t* p1 = a.w1 + (int64_t)min(EPI == OPS_GATE ? f0 + g : f0 + 8 + g, a.n - 1) * a.ld_w + 16 * t;
-  const int whole = a.k_bytes / 64;  // steps of 64 bytes; a ragged rest is the last share's
-  const int per = (whole + a.split - 1) / a.split;
-  const int s0 = min(share * per, whole), s1 = min(s0 + per, whole);
+  const int units = (a.n + FR - 1) / FR;
+  const int mine = ((int)blockIdx.x < units) ? (units - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;
+  // steps of 64 bytes of k, the last one possibly ragged; this warp's are [s0, s1)
+  const int steps = (a.k_bytes + 63) / 64;
+  const int per = (steps + kStreamWarps - 1) / kStreamWarps;
+  const int s0 = min(warp * per, steps), s1 = min(s0 + per, steps);
+  uint8_t* ring = smem + warp * (RING * 1024) + lane * 16;
+  const uint32_t ring_addr = smem_u32(ring);
+  uint8_t* xs = smem + kStreamWarps * RING * 1024;
 
-  uint32_t acc[NT][4];
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0u;
-  uint4 c0[U], c1[U];
-  auto fetch = [&](int s, uint4(&v0)[U], uint4(&v1)[U]) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (s + u < s1) {
-        v0[u] = load_once(p0 + (int64_t)(s + u) * 64);
-        v1[u] = load_once(p1 + (int64_t)(s + u) * 64);
+  // The copies run ahead of the sums through the same sequence: steps s0 .. s1 of the block's first rows, then of its next.
+  int unit = s0 < s1 ? 0 : mine, step = s0, slot = 0;
+  const uint8_t *p0 = nullptr, *p1 = nullptr;
+  auto rows_of = [&](int i) {
+    const int f0 = ((int)blockIdx.x + i * (int)gridDim.x) * FR;
+    p0 = a.w0 + (int64_t)min(f0 + g, a.n - 1) * a.ld_w + 16 * t;
+    p1 = a.w1 + (int64_t)min(EPI == OPS_GATE ? f0 + g : f0 + 8 + g, a.n - 1) * a.ld_w + 16 * t;
+  };
+  auto copy_next = [&]() {
+    if (unit < mine) {
+      const int left = min(max(a.k_bytes - step * 64 - 16 * t, 0), 16);
+      const int64_t at = left ? (int64_t)step * 64 : 0;
+      copy_16(ring_addr + slot * 1024, p0 + at, left);
+      copy_16(ring_addr + slot * 1024 + 512, p1 + at, left);
+      if (++step == s1) {
+        step = s0;
+        if (++unit < mine) rows_of(unit);
       }
+      if (++slot == RING) slot = 0;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto multiply = [&](const uint4& v0, const uint4& v1, const uint4& b, uint32_t(&c)[4]) {
-    mma_16x8<KIND>(c, v0.x, v1.x, v0.y, v1.y, b.x, b.y);
-    mma_16x8<KIND>(c, v0.z, v1.z, v0.w, v1.w, b.z, b.w);
-  };
-
   if (!a.early) grid_dependency_wait();
-  fetch(s0, c0, c1);
+  if (unit < mine) rows_of(0);
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i) copy_next();
   if (a.early) grid_dependency_wait();
   grid_launch_dependents();
 
-  const uint8_t* px[NT];
-  bool have[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    have[i] = g + 8 * i < a.rows;
-    px[i] = a.x + (int64_t)(have[i] ? g + 8 * i : 0) * a.ld_x + 16 * t;
-  }
-  for (int s = s0; s < s1; s += U) {
-    uint4 n0[U], n1[U];
-    fetch(s + U, n0, n1);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (s + u < s1) {
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          uint4 b = make_uint4(0u, 0u, 0u, 0u);
-          if (have[i]) b = *reinterpret_cast<const uint4*>(px[i] + (int64_t)(s + u) * 64);
-          multiply(c0[u], c1[u], b, acc[i]);
-        }
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      c0[u] = n0[u];
-      c1[u] = n1[u];
+  // x: each warp brings its own share of k, so that no barrier is needed
+  for (int r = 0; r < a.rows; ++r) {
+    for (int s = s0 * 4 + lane; s < s1 * 4; s += 32) {
+      const uint8_t* p = a.x + r * a.ld_x + (int64_t)s * 16;
+      const int left = a.k_bytes - s * 16;
+      *reinterpret_cast<uint4*>(xs + r * a.pitch + s * 16) = left >= 16 ? *reinterpret_cast<const uint4*>(p) : load_part(p, left);
     }
   }
-  if (share == a.split - 1 && a.k_bytes % 64) {
-    const int left = a.k_bytes - whole * 64 - 16 * t;
-    const uint4 v0 = load_part(p0 + (int64_t)whole * 64, left), v1 = load_part(p1 + (int64_t)whole * 64, left);
-#pragma unroll
-    for (int i = 0; i < NT; ++i) multiply(v0, v1, load_part(px[i] + (int64_t)whole * 64, have[i] ? left : 0), acc[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    part[warp][8 * i + 2 * t][g] = acc[i][0];
-    part[warp][8 * i + 2 * t + 1][g] = acc[i][1];
-    part[warp][8 * i + 2 * t][g + 8] = acc[i][2];
-    part[warp][8 * i + 2 * t + 1][g + 8] = acc[i][3];
-  }
-  __syncthreads();
+  __syncwarp();
 
-  const int cols = groups * FR;
-  for (int e = threadIdx.x; e < cols * a.rows; e += 32 * kStreamWarps) {
-    const int f = e % cols, row = e / cols, col = blockIdx.x * cols + f;
-    if (col >= a.n) continue;
-    const int w0 = (f / FR) * a.split, r = f % FR;
+  const uint8_t* xr = xs + g * a.pitch + 16 * t;
+  const bool have = g < a.rows;
+  int at = 0;
+  for (int i = 0; i < mine; ++i) {
+    uint32_t acc[4] = {0u, 0u, 0u, 0u};
+    for (int s = s0; s < s1; ++s) {
+      copy_next();  // into the slot of the step before this one
+      asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
+      const uint4 c0 = *reinterpret_cast<const uint4*>(ring + at * 1024), c1 = *reinterpret_cast<const uint4*>(ring + at * 1024 + 512);
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (have) x = *reinterpret_cast<const uint4*>(xr + s * 64);
+      mma_16x8<KIND>(acc, c0.x, c1.x, c0.y, c1.y, x.x, x.y);
+      mma_16x8<KIND>(acc, c0.z, c1.z, c0.w, c1.w, x.z, x.w);
+      if (++at == RING) at = 0;
+    }
+    uint32_t(*p)[8][17] = part[i & 1];  // free: every thread has passed the barrier of unit i - 1 after reading unit i - 2's
+    p[warp][2 * t][g] = acc[0];
+    p[warp][2 * t + 1][g] = acc[1];
+    p[warp][2 * t][g + 8] = acc[2];
+    p[warp][2 * t + 1][g + 8] = acc[3];
+    __syncthreads();
+    const int f = threadIdx.x % FR, row = threadIdx.x / FR, col = ((int)blockIdx.x + i * (int)gridDim.x) * FR + f;
+    if (row >= a.rows || col >= a.n) continue;
     if constexpr (KIND == KIND_I8) {
       int v = 0;
-      for (int s = 0; s < a.split; ++s) v += (int)part[w0 + s][row][r];
+#pragma unroll
+      for (int w = 0; w < kStreamWarps; ++w) v += (int)p[w][row][f];
       const float y = fmaf((float)v * a.scale_a[row], a.scale_b[col], a.bias ? a.bias[col] : 0.f);
       if (a.out_type == ASD_TYPE_F32)
         reinterpret_cast<float*>(a.c)[row * a.ldc + col] = y;
@@ -168,15 +162,16 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 2) stream_kernel(const Stre
         reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(y, a.out_type == ASD_TYPE_F16);
     } else {
       float v = 0.f, u = 0.f;
-      for (int s = 0; s < a.split; ++s) {
-        v += __uint_as_float(part[w0 + s][row][r]);
-        if (EPI == OPS_GATE) u += __uint_as_float(part[w0 + s][row][r + 8]);
+#pragma unroll
+      for (int w = 0; w < kStreamWarps; ++w) {
+        v += __uint_as_float(p[w][row][f]);
+        if (EPI == OPS_GATE) u += __uint_as_float(p[w][row][f + 8]);
       }
       if (EPI == OPS_GATE) {
         if (a.gu) {
           uint8_t* b = a.gu + gu_block_offset(row, col, a.gu_cols);
-          gu_put(b, row & 31, col & 31, v);
-          gu_put(b + kGuHalf, row & 31, col & 31, u);
+          gu_put(b, row, col & 31, v);
+          gu_put(b + kGuHalf, row, col & 31, u);
         }
         v = gate_value(v, a.gelu != 0) * u;
       }
@@ -186,21 +181,35 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 2) stream_kernel(const Stre
 }
 
 template <int KIND, int EPI>
-void launch_nt(const StreamArgs& a, dim3 grid, cudaStream_t st) {
-  const dim3 block(32 * kStreamWarps);
-  if (a.rows <= 8)
-    ops_launch(stream_kernel<KIND, 1, EPI>, grid, block, 0, st, 1, a);
-  else if (a.rows <= 16)
-    ops_launch(stream_kernel<KIND, 2, EPI>, grid, block, 0, st, 1, a);
+void launch_stream(const asd_ops* o, const StreamArgs& a, cudaStream_t st) {
+  const int fr = EPI == OPS_GATE ? 8 : 16;
+  const dim3 grid(std::min((a.n + fr - 1) / fr, o->num_sms)), block(32 * kStreamWarps);
+  const int x = a.rows * a.pitch;  // what x leaves is the ring's
+  if (x <= kStreamSmem - ring_bytes(12))
+    ops_launch(stream_kernel<KIND, EPI, 12>, grid, block, (size_t)(ring_bytes(12) + x), st, 1, a);
+  else if (x <= kStreamSmem - ring_bytes(8))
+    ops_launch(stream_kernel<KIND, EPI, 8>, grid, block, (size_t)(ring_bytes(8) + x), st, 1, a);
   else
-    ops_launch(stream_kernel<KIND, 4, EPI>, grid, block, 0, st, 1, a);
+    ops_launch(stream_kernel<KIND, EPI, 4>, grid, block, (size_t)(ring_bytes(4) + x), st, 1, a);
 }
+template <int KIND, int EPI>
+cudaError_t prepare_stream() {
+  cudaError_t e = cudaFuncSetAttribute(stream_kernel<KIND, EPI, 12>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(stream_kernel<KIND, EPI, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(stream_kernel<KIND, EPI, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+  return e;
+}
+
+// Rows of x lie 64 bytes off a multiple of 128: eight lanes that read two of them meet every bank once.
+int x_pitch(int64_t k_bytes) { return (int)((k_bytes + 127) / 128 * 128 + 64); }
 
 }  // namespace
 
+// Few enough rows, and x fits into shared memory.
 bool use_stream(const OpsGemm& q) {
+  const int es = q.epi == OPS_I8 ? 1 : 2;
   return (q.epi == OPS_GATE || q.epi == OPS_I8 || (q.epi == OPS_STORE && q.parts == 1 && q.groups == 1)) && q.m <= kStreamMaxRows &&
-         !q.a[0].mn && !q.b[0].mn;
+         !q.a[0].mn && !q.b[0].mn && q.m * x_pitch(q.k[0] * es) <= kStreamSmem - ring_bytes(4);
 }
 
 asd_status ops_gemm_stream(const asd_ops* o, const OpsGemm& q, bool early, cudaStream_t st) {
@@ -210,26 +219,27 @@ asd_status ops_gemm_stream(const asd_ops* o, const OpsGemm& q, bool early, cudaS
   a.w1 = (const uint8_t*)q.b[q.epi == OPS_GATE ? 1 : 0].mat.p;
   a.x = (const uint8_t*)q.a[0].mat.p;
   a.ld_w = q.b[0].mat.ld * es, a.ld_x = q.a[0].mat.ld * es;
-  a.rows = (int)q.m, a.n = (int)q.n, a.k_bytes = (int)(q.k[0] * es);
+  a.rows = (int)q.m, a.n = (int)q.n, a.k_bytes = (int)(q.k[0] * es), a.pitch = x_pitch(q.k[0] * es);
   a.early = early;
   a.out_type = q.type, a.gelu = q.act == ASD_ACT_GELU;
   a.c = q.c[0], a.ldc = q.ldc;
   a.gu = q.gu, a.gu_cols = (int)((q.n + 31) / 32);
   a.scale_a = q.scale_a, a.scale_b = q.scale_b, a.bias = q.bias;
-  // as few warps to a k as give two blocks to every SM, and at least 256 bytes of k to a warp
-  const int fr = q.epi == OPS_GATE ? 8 : 16;
-  const int64_t units = (q.n + fr - 1) / fr;
-  a.split = 1;
-  while (a.split < kStreamWarps && units * a.split < 2 * (int64_t)kStreamWarps * o->num_sms && a.k_bytes / (2 * a.split) >= 256) a.split *= 2;
-  const int groups = kStreamWarps / a.split;
-  const dim3 grid((unsigned)((units + groups - 1) / groups));
   if (q.epi == OPS_I8)
-    launch_nt<KIND_I8, OPS_I8>(a, grid, st);
+    launch_stream<KIND_I8, OPS_I8>(o, a, st);
   else if (q.epi == OPS_GATE)
-    q.type == ASD_TYPE_F16 ? launch_nt<KIND_F16, OPS_GATE>(a, grid, st) : launch_nt<KIND_BF16, OPS_GATE>(a, grid, st);
+    q.type == ASD_TYPE_F16 ? launch_stream<KIND_F16, OPS_GATE>(o, a, st) : launch_stream<KIND_BF16, OPS_GATE>(o, a, st);
   else
-    q.type == ASD_TYPE_F16 ? launch_nt<KIND_F16, OPS_STORE>(a, grid, st) : launch_nt<KIND_BF16, OPS_STORE>(a, grid, st);
+    q.type == ASD_TYPE_F16 ? launch_stream<KIND_F16, OPS_STORE>(o, a, st) : launch_stream<KIND_BF16, OPS_STORE>(o, a, st);
   return ops_launched("matrix product of few rows");
+}
+
+asd_status ops_stream_prepare() {
+  const cudaError_t all[] = {prepare_stream<KIND_I8, OPS_I8>(), prepare_stream<KIND_F16, OPS_GATE>(), prepare_stream<KIND_BF16, OPS_GATE>(),
+                             prepare_stream<KIND_F16, OPS_STORE>(), prepare_stream<KIND_BF16, OPS_STORE>()};
+  for (cudaError_t e : all)
+    if (e != cudaSuccess) return ops_fail(ASD_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+  return ASD_OK;
 }
 
 }  // namespace asd

@@ -229,7 +229,7 @@ def test_quantize_edges(ops):
 
 MATMUL_SHAPES = [(1, 1, 1), (1, 64, 128), (2, 4096, 640), (3, 17, 5), (8, 1000, 1001), (15, 129, 255), (16, 2048, 512), (17, 33, 130), (31, 512, 100),
                  (33, 96, 72), (64, 320, 1024), (65, 640, 129), (100, 1111, 77), (128, 256, 256), (129, 4100, 300), (200, 16, 1000), (256, 1024, 256),
-                 (257, 1024, 513), (300, 3000, 1000), (1000, 200, 2000), (2100, 72, 520)]
+                 (257, 1024, 513), (300, 3000, 1000), (1000, 200, 2000), (2100, 72, 520), (5000, 130, 1003), (4100, 257, 2049)]
 
 
 def eight(shape, seed):
@@ -283,7 +283,7 @@ def test_matmul_i8_strides(ops, rows, kind):
 
 MLP_SHAPES = [(1, 64, 128), (1, 8, 8), (1, 1, 1), (2, 5, 3), (3, 130, 77), (7, 1024, 520), (8, 256, 264), (13, 72, 320), (16, 512, 1000), (17, 33, 65),
               (32, 320, 640), (40, 1000, 136), (64, 128, 512), (65, 264, 129), (128, 256, 384), (130, 1001, 259), (256, 256, 256), (300, 72, 1000),
-              (600, 520, 777), (1030, 129, 300), (2048, 512, 512)]
+              (600, 520, 777), (1030, 129, 300), (2048, 512, 512), (5000, 72, 1001), (4097, 257, 640)]
 
 
 def mlp_data(rows, width, hidden, t):
