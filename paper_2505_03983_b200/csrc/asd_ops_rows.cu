@@ -3,7 +3,7 @@
 // matrix product.
 //
 // All of them are bound by memory: a row is read once, kept in registers over its reductions, and written once.  A row
-// belongs to 32, 128 or 512 threads (rows of up to 1024, 4096, 16384), 32 elements to a thread, so that a thread has its
+// belongs to 32, 128, 256 or 512 threads (rows of up to 1024, 4096, 8192, 16384), 32 elements to a thread, so that a thread has its
 // 16-byte loads in flight together; longer rows are read a second time.  A row whose address, distance or length is not a
 // multiple of 8 elements is read element by element, neighbouring threads on neighbouring elements.
 #include <float.h>
@@ -66,21 +66,28 @@ __device__ __forceinline__ void store_vec(T* p, const float (&f)[VEC]) {
     *reinterpret_cast<uint4*>(p) = v;
   }
 }
+// q = rint(f inv), |f inv| <= 127.  Adding 1.5 2^23 rounds to the nearest even integer and leaves it, as two's complement, in
+// the low bits of the sum: three byte selections pack four of them, where conversions would take one slow instruction each.
+__device__ __forceinline__ uint32_t rounded_bits(float f, float inv) { return __float_as_uint(fmaf(f, inv, 12582912.f)); }
 template <int VEC>
 __device__ __forceinline__ void store_q(int8_t* p, const float (&f)[VEC], float inv) {
   if constexpr (VEC == 1) {
-    *p = (int8_t)__float2int_rn(f[0] * inv);
+    *p = (int8_t)rounded_bits(f[0], inv);
   } else {
     uint32_t w[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t b[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = (uint32_t)__float2int_rn(f[4 * h + i] * inv) & 0xffu;
-      w[h] = b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24);
-    }
+    for (int h = 0; h < 2; ++h)
+      w[h] = __byte_perm(__byte_perm(rounded_bits(f[4 * h], inv), rounded_bits(f[4 * h + 1], inv), 0x0040),
+                         __byte_perm(rounded_bits(f[4 * h + 2], inv), rounded_bits(f[4 * h + 3], inv), 0x0040), 0x5410);
     *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
   }
+}
+template <int VEC>
+__device__ __forceinline__ void store_zero(int8_t* p) {
+  if constexpr (VEC == 1)
+    *p = 0;
+  else
+    *reinterpret_cast<uint2*>(p) = make_uint2(0u, 0u);
 }
 template <int VEC, typename T>
 __device__ __forceinline__ void load_weight(const void* w, int w_f32, int col, float (&f)[VEC]) {
@@ -128,15 +135,29 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* buf) {
 __device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 struct RowScale {
   float inv, scale;  // q = rint(y inv), y ~ q scale
+  bool ok;           // false: the row has a NaN or an infinity; q = 0
 };
 __device__ __forceinline__ RowScale row_scale(uint32_t most) {
-  if (most >= 0x7f800000u) return {0.f, __uint_as_float(0x7fffffffu)};
+  if (most >= 0x7f800000u) return {0.f, __uint_as_float(0x7fffffffu), false};
   const float m = fmaxf(__uint_as_float(most), kTiny);
-  return {127.f / m, m / 127.f};
+  return {127.f / m, m / 127.f, true};
+}
+template <int VEC>
+__device__ __forceinline__ void put_q(int8_t* p, const float (&f)[VEC], const RowScale& rs) {
+  if (rs.ok)
+    store_q<VEC>(p, f, rs.inv);
+  else
+    store_zero<VEC>(p);
 }
 
+// The exponential and the reciprocal are the approximate instructions (relative error some 2^-22).
 __device__ __forceinline__ float act_value(float g, int act) {
-  if (act == ASD_ACT_SILU) return g * (1.f / (1.f + __expf(-g)));
+  if (act == ASD_ACT_SILU) {
+    float e, p;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(1.f + e));
+    return g * p;
+  }
   return 0.5f * g * (1.f + erff(g * 0.7071067811865476f));
 }
 
@@ -219,7 +240,7 @@ __global__ void __launch_bounds__(block_of<TPR>) rmsnorm_kernel(const NormArgs a
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int col = (v * TPR + t) * VEC;
-        if (col < a.width) store_q<VEC>(y + col, f[v], rs.inv);
+        if (col < a.width) put_q<VEC>(y + col, f[v], rs);
       }
       if (t == 0) a.scale[row] = rs.scale;
     }
@@ -261,7 +282,7 @@ __global__ void __launch_bounds__(block_of<TPR>) rmsnorm_kernel(const NormArgs a
       for (int col = t * VEC; col < a.width; col += TPR * VEC) {
         float f[VEC];
         again(col, f);
-        store_q<VEC>(reinterpret_cast<int8_t*>(a.y) + row * a.ld_y + col, f, rs.inv);
+        put_q<VEC>(reinterpret_cast<int8_t*>(a.y) + row * a.ld_y + col, f, rs);
       }
       if (t == 0) a.scale[row] = rs.scale;
     }
@@ -312,7 +333,7 @@ __global__ void __launch_bounds__(block_of<TPR>) quantize_kernel(const QuantArgs
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int col = (v * TPR + t) * VEC;
-      if (col < a.width) store_q<VEC>(q + col, f[v], rs.inv);
+      if (col < a.width) put_q<VEC>(q + col, f[v], rs);
     }
     if (t == 0) a.scale[row] = rs.scale;
   } else {
@@ -326,7 +347,7 @@ __global__ void __launch_bounds__(block_of<TPR>) quantize_kernel(const QuantArgs
     for (int col = t * VEC; col < a.width; col += TPR * VEC) {
       float f[VEC];
       fetch(col, f);
-      store_q<VEC>(q + col, f, rs.inv);
+      put_q<VEC>(q + col, f, rs);
     }
     if (t == 0) a.scale[row] = rs.scale;
   }
@@ -342,9 +363,35 @@ struct NormGradArgs {
   int64_t ld_dy, ld_s, ld_ds, ld_dx;
 };
 
+// VEC elements as they are stored.
+template <typename T, int VEC>
+struct RawVec {
+  uint4 v[sizeof(T) * VEC / 16];
+};
+template <typename T>
+struct RawVec<T, 1> {
+  T v[1];
+};
+template <int VEC, typename T>
+__device__ __forceinline__ RawVec<T, VEC> load_raw(const T* p) {
+  RawVec<T, VEC> r;
+  if constexpr (VEC == 1) {
+    r.v[0] = *p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r.v) / 16); ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  return r;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ float raw_at(const RawVec<T, VEC>& r, int i) {
+  return to_f<T>(reinterpret_cast<const T*>(&r.v[0])[i]);
+}
+
 // Gradients.  One block walks over rows blockIdx.x, + blocks, ...; a thread keeps the same columns in every row, so the
-// sums of dw over the block's rows stay in its registers and are written once, to be added up by reduce_dw_kernel.  Both
-// sums of a row, of s^2 and of dy w s, are taken together: mean(dy w z) = rho mean(dy w s).
+// weights and the sums of dw over the block's rows stay in its registers; the sums are written once, to be added up by
+// reduce_dw_kernel.  Both sums of a row, of s^2 and of dy w s, are taken together: mean(dy w z) = rho mean(dy w s).  The next
+// row's loads (kept as they are stored) are issued before a row's sums meet, so that memory is busy over the barrier.
 template <typename T, int VEC, int TPR, int PER>
 __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a) {
   constexpr int NV = PER / VEC;
@@ -352,38 +399,45 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
   dep_wait();
   dep_launch();
   const int t = threadIdx.x;
-  float acc[NV][VEC];
+  float acc[NV][VEC], w[NV][VEC];
 #pragma unroll
-  for (int v = 0; v < NV; ++v)
+  for (int v = 0; v < NV; ++v) {
+    const int col = (v * TPR + t) * VEC;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) acc[v][i] = 0.f;
-  int turn = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks, turn ^= 1) {
-    const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.ld_dy;
+    for (int i = 0; i < VEC; ++i) acc[v][i] = w[v][i] = 0.f;
+    if (col < a.width) load_weight<VEC, T>(a.w, a.w_f32, col, w[v]);
+  }
+  struct Row {
+    RawVec<T, VEC> s[NV], dy[NV], ds[NV];
+  };
+  auto fetch = [&](int64_t row, Row& r) {
     const T* s = reinterpret_cast<const T*>(a.s) + row * a.ld_s;
-    float g[NV][VEC], f[NV][VEC];
+    const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.ld_dy;
+    const T* ds = reinterpret_cast<const T*>(a.ds) + row * a.ld_ds;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int col = (v * TPR + t) * VEC;
       if (col < a.width) {
-        load_vec<VEC, T>(s + col, f[v]);
-        load_vec<VEC, T>(dy + col, g[v]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) f[v][i] = g[v][i] = 0.f;
+        r.s[v] = load_raw<VEC, T>(s + col);
+        r.dy[v] = load_raw<VEC, T>(dy + col);
+        if (a.ds) r.ds[v] = load_raw<VEC, T>(ds + col);
       }
     }
+  };
+  Row cur, next;
+  int turn = 0;
+  if (blockIdx.x < a.rows) fetch(blockIdx.x, cur);
+  for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks, turn ^= 1) {
+    if (row + a.blocks < a.rows) fetch(row + a.blocks, next);
     float sq = 0.f, dot = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * TPR + t) * VEC;
-      if (col < a.width) {
-        float w[VEC];
-        load_weight<VEC, T>(a.w, a.w_f32, col, w);
+      if ((v * TPR + t) * VEC < a.width) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          sq = fmaf(f[v][i], f[v][i], sq);
-          dot = fmaf(g[v][i] * w[i], f[v][i], dot);
+          const float f = raw_at(cur.s[v], i);
+          sq = fmaf(f, f, sq);
+          dot = fmaf(raw_at(cur.dy[v], i) * w[v][i], f, dot);
         }
       }
     }
@@ -406,19 +460,18 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
     for (int v = 0; v < NV; ++v) {
       const int col = (v * TPR + t) * VEC;
       if (col < a.width) {
-        float w[VEC], d[VEC], e[VEC];
-        load_weight<VEC, T>(a.w, a.w_f32, col, w);
-        if (a.ds) load_vec<VEC, T>(reinterpret_cast<const T*>(a.ds) + row * a.ld_ds + col, e);
+        float d[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          const float z = f[v][i] * rho;
-          acc[v][i] = fmaf(g[v][i], z, acc[v][i]);
-          d[i] = rho * (g[v][i] * w[i] - z * c);
-          if (a.ds) d[i] += e[i];
+          const float z = raw_at(cur.s[v], i) * rho, g = raw_at(cur.dy[v], i);
+          acc[v][i] = fmaf(g, z, acc[v][i]);
+          d[i] = rho * (g * w[v][i] - z * c);
+          if (a.ds) d[i] += raw_at(cur.ds[v], i);
         }
         if (a.dx) store_vec<VEC, T>(reinterpret_cast<T*>(a.dx) + row * a.ld_dx + col, d);
       }
     }
+    cur = next;
   }
   if (a.part) {
 #pragma unroll
@@ -432,7 +485,7 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
   }
 }
 
-// Rows of more than 16384: dx row by row with rho kept per row, the sums of dw by columns afterwards.
+// Rows of more than 8192: dx row by row with rho kept per row, the sums of dw by columns afterwards.
 template <typename T>
 __global__ void __launch_bounds__(512) rmsnorm_grad_long_kernel(const NormGradArgs a) {
   __shared__ float buf[2][16];
@@ -486,8 +539,10 @@ __global__ void __launch_bounds__(1024) reduce_dw_kernel(const float* part, int 
   dep_launch();
   const int col = blockIdx.x * 32 + threadIdx.x;
   float acc = 0.f;
-  if (col < width)
+  if (col < width) {
+#pragma unroll 8
     for (int b = threadIdx.y; b < blocks; b += 32) acc += part[(size_t)b * width + col];
+  }
   buf[threadIdx.y][threadIdx.x] = acc;
   __syncthreads();
   const float v = warp_sum(buf[threadIdx.x][threadIdx.y]);
@@ -511,6 +566,7 @@ bool aligned(const void* p, int64_t ld, int es, int bytes) { return ((uintptr_t)
 int row_threads(const asd_ops* o, int64_t rows, int width) {
   if (width <= 32 * kPer && (width <= 256 || rows >= 8 * o->num_sms)) return 32;
   if (width <= 128 * kPer && (width <= 1024 || rows >= 4 * o->num_sms)) return 128;
+  if (width <= 256 * kPer && rows >= 2 * o->num_sms) return 256;
   return 512;
 }
 
@@ -521,6 +577,8 @@ void rmsnorm_t(const asd_ops* o, const NormArgs& n, cudaStream_t st) {
     ops_launch(rmsnorm_kernel<T, VEC, 32, Q8, false>, dim3((n.rows + 3) / 4), dim3(128), 0, st, 1, n);
   else if (tpr == 128)
     ops_launch(rmsnorm_kernel<T, VEC, 128, Q8, false>, dim3(n.rows), dim3(128), 0, st, 1, n);
+  else if (tpr == 256)
+    ops_launch(rmsnorm_kernel<T, VEC, 256, Q8, false>, dim3(n.rows), dim3(256), 0, st, 1, n);
   else if (n.width <= 512 * kPer)
     ops_launch(rmsnorm_kernel<T, VEC, 512, Q8, false>, dim3(n.rows), dim3(512), 0, st, 1, n);
   else
@@ -541,16 +599,19 @@ void quantize_t(const asd_ops* o, const QuantArgs& n, cudaStream_t st) {
     ops_launch(quantize_kernel<T, VEC, 32, false>, dim3((n.rows + 3) / 4), dim3(128), 0, st, 1, n);
   else if (tpr == 128)
     ops_launch(quantize_kernel<T, VEC, 128, false>, dim3(n.rows), dim3(128), 0, st, 1, n);
+  else if (tpr == 256)
+    ops_launch(quantize_kernel<T, VEC, 256, false>, dim3(n.rows), dim3(256), 0, st, 1, n);
   else if (n.width <= 512 * kPer)
     ops_launch(quantize_kernel<T, VEC, 512, false>, dim3(n.rows), dim3(512), 0, st, 1, n);
   else
     ops_launch(quantize_kernel<T, VEC, 512, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
 }
 
-// Blocks of the gradient: enough to fill the SMs, few enough that their partial sums of dw stay a small share of the
-// traffic.
+constexpr int kGradWidth = 8192;  // the longest row whose sums of dw a block keeps in registers
+// Blocks of the gradient: as many as the SMs hold together, so that each block's sums of dw are over as many rows as
+// possible.
 int grad_blocks(const asd_ops* o, int64_t rows, int width) {
-  const int per_sm = width <= 1024 ? 8 : width <= 4096 ? 3 : width <= 16384 ? 1 : 2;
+  const int per_sm = width <= 1024 ? 8 : width <= 4096 ? 2 : width <= kGradWidth ? 1 : 2;
   const int64_t most = (int64_t)per_sm * o->num_sms;
   return (int)(rows < most ? rows : most);
 }
@@ -560,8 +621,8 @@ void grad_t(const asd_ops* o, const NormGradArgs& n, cudaStream_t st) {
     ops_launch(rmsnorm_grad_kernel<T, VEC, 64, 16>, dim3(n.blocks), dim3(64), 0, st, 1, n);
   else if (n.width <= 4096)
     ops_launch(rmsnorm_grad_kernel<T, VEC, 256, 16>, dim3(n.blocks), dim3(256), 0, st, 1, n);
-  else if (n.width <= 16384)
-    ops_launch(rmsnorm_grad_kernel<T, VEC, 512, 32>, dim3(n.blocks), dim3(512), 0, st, 1, n);
+  else if (n.width <= kGradWidth)
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 512, 16>, dim3(n.blocks), dim3(512), 0, st, 1, n);
   else {
     ops_launch(rmsnorm_grad_long_kernel<T>, dim3(n.rows), dim3(512), 0, st, 1, n);
     if (n.part) ops_launch(columns_dw_kernel<T>, dim3((n.width + 127) / 128, n.blocks), dim3(128), 0, st, 1, n);
@@ -602,7 +663,7 @@ void launch_quantize(const asd_ops* o, const asd_quantize_args* a, cudaStream_t 
 
 int64_t rmsnorm_backward_bytes(const asd_ops* o, const asd_rmsnorm_backward_args* a) {
   if (!a->dw || a->rows == 0) return 0;
-  return 4 * ((int64_t)grad_blocks(o, a->rows, a->width) * a->width + (a->width > 16384 ? a->rows : 0));
+  return 4 * ((int64_t)grad_blocks(o, a->rows, a->width) * a->width + (a->width > kGradWidth ? a->rows : 0));
 }
 
 void launch_rmsnorm_backward(const asd_ops* o, const asd_rmsnorm_backward_args* a, cudaStream_t st) {
