@@ -30,12 +30,14 @@ struct Cut {
 };
 
 // An operand of a matrix product as the TMA can read it: itself, or a copy in the workspace with rows of a multiple of
-// 16 bytes.  `launch` false only sizes the workspace.
-Mat aligned_operand(const asd_ops* o, Mat m, Cut* cut, bool launch, cudaStream_t st) {
+// 16 bytes, which is added to the list of copies to be made.
+Mat aligned_operand(Mat m, Cut* cut, Packs* packs) {
   if (mat_aligned(m)) return m;
   const int64_t ld = round_up(m.cols * m.es, 16) / m.es;
   void* p = cut->take(m.rows * ld * m.es);
-  if (launch) launch_pack(o, m, p, ld, st);
+  packs->src[packs->n] = m;
+  packs->dst[packs->n] = p;
+  packs->ld[packs->n++] = ld;
   return Mat{p, m.rows, m.cols, ld, m.es};
 }
 
@@ -98,12 +100,15 @@ asd_status check_matmul(const asd_ops* o, const asd_matmul_i8_args* a) {
 }
 asd_status run_matmul(const asd_ops* o, const asd_matmul_i8_args* a, Cut* cut, bool launch, cudaStream_t st) {
   OpsGemm g{};
-  g.epi = OPS_I8, g.type = a->out_type, g.m = a->rows, g.n = a->out, g.k[0] = a->k, g.parts = g.groups = 1;
-  g.a[0] = {aligned_operand(o, Mat{a->a, a->rows, a->k, a->ld_a, 1}, cut, launch, st), false};
-  g.b[0] = {aligned_operand(o, Mat{a->b, a->out, a->k, a->ld_b, 1}, cut, launch, st), false};
+  Packs packs;
+  g.epi = OPS_I8, g.type = a->out_type, g.m = a->rows, g.n = a->out, g.k[0] = a->k, g.parts = 1;
+  g.a[0] = {aligned_operand(Mat{a->a, a->rows, a->k, a->ld_a, 1}, cut, &packs), false};
+  g.b[0] = {aligned_operand(Mat{a->b, a->out, a->k, a->ld_b, 1}, cut, &packs), false};
+  if (!launch) return ASD_OK;
+  launch_packs(o, packs, st);
   g.c[0] = a->y, g.ldc = a->ld_y;
   g.scale_a = a->a_scale, g.scale_b = a->b_scale, g.bias = a->bias;
-  return launch ? ops_gemm(o, g, false, st) : ASD_OK;
+  return ops_gemm(o, g, false, st);
 }
 
 // ---- gated_mlp ----------------------------------------------------------------------------------------
@@ -117,26 +122,28 @@ asd_status check_mlp(int32_t rows, int32_t width, int32_t hidden, int32_t type, 
   return ASD_OK;
 }
 int64_t padded_hidden(int64_t hidden) { return round_up(hidden, 8); }
-// saved: h [rows, padded hidden], then g and u
+// saved: h [rows, padded hidden], then the gate's two factors
 int64_t saved_h_bytes(int64_t rows, int64_t hidden) { return round_up(rows * padded_hidden(hidden) * 2, 256); }
 
 asd_status run_forward(const asd_ops* o, const asd_gated_mlp_args* a, Cut* cut, bool launch, cudaStream_t st) {
   const int64_t hp = padded_hidden(a->hidden);
-  const Mat x = aligned_operand(o, Mat{a->x, a->rows, a->width, a->ld_x, 2}, cut, launch, st);
-  const Mat w = aligned_operand(o, Mat{a->w_in, 2 * (int64_t)a->hidden, a->width, a->ld_w_in, 2}, cut, launch, st);
-  const Mat wo = aligned_operand(o, Mat{a->w_out, a->width, a->hidden, a->ld_w_out, 2}, cut, launch, st);
+  Packs packs;
+  const Mat x = aligned_operand(Mat{a->x, a->rows, a->width, a->ld_x, 2}, cut, &packs);
+  const Mat w = aligned_operand(Mat{a->w_in, 2 * (int64_t)a->hidden, a->width, a->ld_w_in, 2}, cut, &packs);
+  const Mat wo = aligned_operand(Mat{a->w_out, a->width, a->hidden, a->ld_w_out, 2}, cut, &packs);
   void* h = a->saved ? a->saved : cut->take(a->rows * hp * 2);
   if (!launch) return ASD_OK;
+  launch_packs(o, packs, st);
   OpsGemm g{};
-  g.epi = OPS_GATE, g.type = a->type, g.act = a->act, g.m = a->rows, g.n = a->hidden, g.k[0] = a->width, g.parts = g.groups = 1;
+  g.epi = OPS_GATE, g.type = a->type, g.act = a->act, g.m = a->rows, g.n = a->hidden, g.k[0] = a->width, g.parts = 1;
   g.a[0] = {x, false};
   g.b[0] = {Mat{w.p, a->hidden, w.cols, w.ld, 2}, false};
   g.b[1] = {Mat{(const uint8_t*)w.p + 2 * w.ld * a->hidden, a->hidden, w.cols, w.ld, 2}, false};
   g.c[0] = h, g.ldc = hp;
-  g.gu = a->saved ? (uint8_t*)a->saved + saved_h_bytes(a->rows, a->hidden) : nullptr;
+  g.kept = a->saved ? (uint8_t*)a->saved + saved_h_bytes(a->rows, a->hidden) : nullptr;
   CHECK(ops_gemm(o, g, false, st));
   OpsGemm y{};
-  y.epi = OPS_STORE, y.type = a->type, y.m = a->rows, y.n = a->width, y.k[0] = a->hidden, y.parts = y.groups = 1;
+  y.epi = OPS_STORE, y.type = a->type, y.m = a->rows, y.n = a->width, y.k[0] = a->hidden, y.parts = 1;
   y.a[0] = {Mat{h, a->rows, a->hidden, hp, 2}, false};
   y.b[0] = {wo, false};
   y.c[0] = a->y, y.ldc = a->ld_y;
@@ -146,49 +153,46 @@ asd_status run_forward(const asd_ops* o, const asd_gated_mlp_args* a, Cut* cut, 
 asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, Cut* cut, bool launch, cudaStream_t st) {
   const int64_t hp = padded_hidden(a->hidden), rows = a->rows;
   const bool inner = a->dx || a->dw_in;
-  const Mat dy = aligned_operand(o, Mat{a->dy, rows, a->width, a->ld_dy, 2}, cut, launch, st);
+  Packs packs;
+  const Mat dy = aligned_operand(Mat{a->dy, rows, a->width, a->ld_dy, 2}, cut, &packs);
   Mat x{}, w{}, wo{};
-  if (a->dw_in) x = aligned_operand(o, Mat{a->x, rows, a->width, a->ld_x, 2}, cut, launch, st);
-  if (a->dx) w = aligned_operand(o, Mat{a->w_in, 2 * (int64_t)a->hidden, a->width, a->ld_w_in, 2}, cut, launch, st);
-  if (inner) wo = aligned_operand(o, Mat{a->w_out, a->width, a->hidden, a->ld_w_out, 2}, cut, launch, st);
+  if (a->dw_in) x = aligned_operand(Mat{a->x, rows, a->width, a->ld_x, 2}, cut, &packs);
+  if (a->dx) w = aligned_operand(Mat{a->w_in, 2 * (int64_t)a->hidden, a->width, a->ld_w_in, 2}, cut, &packs);
+  if (inner) wo = aligned_operand(Mat{a->w_out, a->width, a->hidden, a->ld_w_out, 2}, cut, &packs);
   uint8_t* dgu = inner ? (uint8_t*)cut->take(rows * 2 * hp * 2) : nullptr;  // [rows, dg | du], each padded
   if (!launch) return ASD_OK;
+  launch_packs(o, packs, st);
   const Mat dg{dgu, rows, a->hidden, 2 * hp, 2}, du{dgu + 2 * hp, rows, a->hidden, 2 * hp, 2};
   if (inner) {  // dh = dy w_out, and from it dg and du
     OpsGemm g{};
-    g.epi = OPS_GATE_GRAD, g.type = a->type, g.act = a->act, g.m = rows, g.n = a->hidden, g.k[0] = a->width, g.parts = g.groups = 1;
+    g.epi = OPS_GATE_GRAD, g.type = a->type, g.m = rows, g.n = a->hidden, g.k[0] = a->width, g.parts = 1;
     g.a[0] = {dy, false};
     g.b[0] = {wo, true};
     g.c[0] = dgu, g.c[1] = dgu + 2 * hp, g.ldc = 2 * hp;
-    g.gu = (uint8_t*)a->saved + saved_h_bytes(rows, a->hidden);
+    g.kept = (uint8_t*)a->saved + saved_h_bytes(rows, a->hidden);
     CHECK(ops_gemm(o, g, false, st));
   }
-  if (a->dw_out) {  // dy^T h
+  OpsGemm list[kMostProducts];
+  int n = 0;
+  auto product = [&](const Operand& p, const Operand& q, void* c, int64_t ldc, int64_t m, int64_t cols, int64_t k) -> OpsGemm& {
     OpsGemm g{};
-    g.epi = OPS_STORE, g.type = a->type, g.m = a->width, g.n = a->hidden, g.k[0] = rows, g.parts = g.groups = 1;
-    g.a[0] = {dy, true};
-    g.b[0] = {Mat{a->saved, rows, a->hidden, hp, 2}, true};
-    g.c[0] = a->dw_out, g.ldc = a->ld_dw_out;
-    CHECK(ops_gemm(o, g, false, st));
-  }
+    g.epi = OPS_STORE, g.type = a->type, g.m = m, g.n = cols, g.k[0] = k, g.parts = 1;
+    g.a[0] = p, g.b[0] = q, g.c[0] = c, g.ldc = ldc;
+    return list[n++] = g;
+  };
   if (a->dx) {  // dg Wg + du Wu
-    OpsGemm g{};
-    g.epi = OPS_STORE, g.type = a->type, g.m = rows, g.n = a->width, g.k[0] = g.k[1] = a->hidden, g.parts = 2, g.groups = 1;
-    g.a[0] = {dg, false}, g.a[1] = {du, false};
-    g.b[0] = {Mat{w.p, a->hidden, w.cols, w.ld, 2}, true};
+    OpsGemm& g = product({dg, false}, {Mat{w.p, a->hidden, w.cols, w.ld, 2}, true}, a->dx, a->ld_dx, rows, a->width, a->hidden);
+    g.parts = 2, g.k[1] = a->hidden;
+    g.a[1] = {du, false};
     g.b[1] = {Mat{(const uint8_t*)w.p + 2 * w.ld * a->hidden, a->hidden, w.cols, w.ld, 2}, true};
-    g.c[0] = a->dx, g.ldc = a->ld_dx;
-    CHECK(ops_gemm(o, g, false, st));
   }
-  if (a->dw_in) {  // dg^T x and du^T x
-    OpsGemm g{};
-    g.epi = OPS_STORE, g.type = a->type, g.m = a->hidden, g.n = a->width, g.k[0] = rows, g.parts = 1, g.groups = 2;
-    g.a[0] = {dg, true}, g.a[1] = {du, true};
-    g.b[0] = g.b[1] = {x, true};
-    g.c[0] = a->dw_in, g.c[1] = (uint8_t*)a->dw_in + 2 * a->ld_dw_in * a->hidden, g.ldc = a->ld_dw_in;
-    CHECK(ops_gemm(o, g, false, st));
+  if (a->dw_in) {  // dg^T x, du^T x
+    product({dg, true}, {x, true}, a->dw_in, a->ld_dw_in, a->hidden, a->width, rows);
+    product({du, true}, {x, true}, (uint8_t*)a->dw_in + 2 * a->ld_dw_in * a->hidden, a->ld_dw_in, a->hidden, a->width, rows);
   }
-  return ASD_OK;
+  if (a->dw_out)  // dy^T h
+    product({dy, true}, {Mat{a->saved, rows, a->hidden, hp, 2}, true}, a->dw_out, a->ld_dw_out, a->width, a->hidden, rows);
+  return ops_gemm_list(o, list, n, st);
 }
 
 asd_status check_forward(const asd_ops* o, const asd_gated_mlp_args* a) {
@@ -281,6 +285,7 @@ asd_status asd_ops_create(asd_ops** out) {
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return ops_fail(ASD_ERR_CUDA, "cudaDeviceGetAttribute: %s", cudaGetErrorString(cudaGetLastError()));
   REQUIRE(major == 10, ASD_ERR_UNSUPPORTED, "the library is built for sm_100a; device %d has compute capability %d.x", dev, major);
+  CHECK(ops_rows_prepare());
   CHECK(ops_gemm_prepare());
   CHECK(ops_stream_prepare());
   CHECK(ops_split_prepare());
@@ -394,7 +399,7 @@ asd_status asd_gated_mlp_saved(asd_ops* o, const asd_gated_mlp_args* a, int64_t*
   REQUIRE(bytes, ASD_ERR_INVALID_ARG, "bytes must not be NULL");
   CHECK(check_handle(o, a));
   CHECK(check_mlp(a->rows, a->width, a->hidden, a->type, a->act));
-  *bytes = saved_h_bytes(a->rows, a->hidden) + gated_saved_gu_bytes(a->rows, a->hidden);
+  *bytes = saved_h_bytes(a->rows, a->hidden) + gated_kept_bytes(a->rows, a->hidden);
   return ASD_OK;
 }
 asd_status asd_gated_mlp_forward_workspace(asd_ops* o, const asd_gated_mlp_args* a, int64_t* bytes) {

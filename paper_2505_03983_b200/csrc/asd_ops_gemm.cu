@@ -12,11 +12,12 @@
 // Epilogues, on the fp32 (8-bit products: int32) accumulator:
 //   STORE      C rounded to 16 bits
 //   GATE       the tile holds BN / 2 columns of g and the same columns of u (one CTA of the pair loads the gate's weights,
-//              the other the value's): h = act(g) u, and g and u kept for the backward pass
-//   GATE_GRAD  C = dh: dg = dh u act'(g), du = dh act(g)
+//              the other the value's): h = act(g) u, and its two derivatives kept for the backward pass
+//   GATE_GRAD  C = dh: dg = dh u act'(g), du = dh act(g), from the two factors that were kept
 //   I8         C scale_a[m] scale_b[n] + bias[n], rounded to the output's type
 // An output whose address and row distance are multiples of 16 bytes leaves through shared memory by TMA stores of 128-byte
 // row pieces; the others are staged in the same way and stored by lanes on neighbouring elements.
+#include <limits.h>
 #include <string.h>
 
 #include <algorithm>
@@ -35,28 +36,40 @@ namespace {
 constexpr int kStoreBytes = 32 * 128;  // a warp's staging buffer: 32 rows of 128 bytes
 constexpr int kBand = 8;               // tile rows that are walked over together
 
-struct PairMaps {
-  CUtensorMap a[2], b[2], c[2];
-};
-struct PairArgs {
+// One product of a launch.
+struct PairProduct {
   int m, n;       // of C (GATE: n = hidden)
-  int kb[2];      // k-blocks of the first and of the second sum (parts)
-  int groups;     // products side by side
+  int kb[2];      // k-blocks of the first and of the second sum
   int tiles_m, tiles_n;
+  int first;      // number of its first tile in the launch
   int a_mn, b_mn;
   uint32_t idesc;
+  int tma_store;
+  void* c;
+  int64_t ldc;
+};
+template <int N>
+struct PairMaps {
+  struct One {
+    CUtensorMap a[2], b[2], c[2];
+  } p[N];
+};
+template <int N>
+struct PairArgs {
+  PairProduct p[N];
+  int tiles;      // of all products
   int out_type;   // asd_type
   int gelu;
-  int tma_store;
-  void* c[2];
-  int64_t ldc;
-  uint8_t* gu;
-  int gu_cols;    // blocks of 32 columns
+  uint8_t* kept;
+  int kept_cols;  // blocks of 32 columns
   const float* scale_a;
   const float* scale_b;
   const float* bias;
   int* err;
 };
+// OPS_STORE products come in lists.
+template <int EPI>
+constexpr int products_of = EPI == OPS_STORE ? kMostProducts : 1;
 
 template <int BN, int EPI>
 struct OpPairCfg {
@@ -123,16 +136,18 @@ __device__ __forceinline__ void stage_half(uint8_t* buf, int lane, int half, con
 }
 
 struct Tile {
-  int group, m0, n0;
+  int product, m0, n0;
 };
-template <int BN>
-__device__ __forceinline__ Tile tile_at(const PairArgs& g, int t) {
-  const int per = g.tiles_m * g.tiles_n;
+template <int BN, int N>
+__device__ __forceinline__ Tile tile_at(const PairArgs<N>& g, int t) {
   Tile r;
-  r.group = t >= per ? 1 : 0;
-  t -= r.group * per;
-  const int band = t / (kBand * g.tiles_n), first = band * kBand;
-  const int rows = min(g.tiles_m - first, kBand), in = t - first * g.tiles_n;
+  r.product = 0;
+  for (int i = 1; i < N; ++i)
+    if (t >= g.p[i].first) r.product = i;
+  const PairProduct& p = g.p[r.product];
+  t -= p.first;
+  const int band = t / (kBand * p.tiles_n), first = band * kBand;
+  const int rows = min(p.tiles_m - first, kBand), in = t - first * p.tiles_n;
   r.m0 = (first + in % rows) * 2 * BM;
   r.n0 = (in / rows) * BN;
   return r;
@@ -140,7 +155,7 @@ __device__ __forceinline__ Tile tile_at(const PairArgs& g, int t) {
 
 template <int BN, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ PairArgs g) {
+op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __grid_constant__ PairArgs<products_of<EPI>> g) {
   using C = OpPairCfg<BN, EPI>;
   constexpr int S = C::kStages;
   constexpr bool I8 = EPI == OPS_I8;
@@ -163,13 +178,12 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
-  const int num_kb = g.kb[0] + g.kb[1];
-  const int n_tiles = g.groups * g.tiles_m * g.tiles_n;
+  const int n_tiles = g.tiles;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      prefetch_tmap(&maps.a[i]);
-      prefetch_tmap(&maps.b[i]);
+      prefetch_tmap(&maps.p[0].a[i]);
+      prefetch_tmap(&maps.p[0].b[i]);
     }
     for (int s = 0; s < S; ++s) {
       mbar_init(full_bar(s), 1);
@@ -204,25 +218,29 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
       uint32_t phase = 0;
       for (int t = pair; t < n_tiles; t += n_pairs) {
         const Tile tile = tile_at<CN>(g, t);
+        const PairProduct& p = g.p[tile.product];
+        const auto& mp = maps.p[tile.product];
+        const int num_kb = p.kb[0] + p.kb[1];
+        const bool a_mn = p.a_mn, b_mn = p.b_mn;
         const int m0 = tile.m0 + (int)rank * BM;
         const int n0 = EPI == OPS_GATE ? tile.n0 : tile.n0 + (int)rank * (BN / 2);
         for (int kb = 0; kb < num_kb; ++kb) {
-          const int part = kb >= g.kb[0] ? 1 : 0;
-          const int k0 = (kb - part * g.kb[0]) * (I8 ? 128 : 64);
-          const CUtensorMap* ma = &maps.a[part | tile.group];
-          const CUtensorMap* mb = &maps.b[EPI == OPS_GATE ? (int)rank : (part | tile.group)];
+          const int part = kb >= p.kb[0] ? 1 : 0;
+          const int k0 = (kb - part * p.kb[0]) * (I8 ? 128 : 64);
+          const CUtensorMap* ma = &mp.a[part];
+          const CUtensorMap* mb = &mp.b[EPI == OPS_GATE ? (int)rank : part];
           mbar_wait(empty_bar(stage), phase ^ 1u, dead, g.err);
           const uint32_t sa = tiles + stage * C::kStageBytes;
           const uint32_t sb = sa + BM * 128;
           const uint32_t full0 = map_to_cta(full_bar(stage), 0);
           if (rank == 0) mbar_expect_tx(full_bar(stage), 2u * (uint32_t)C::kStageBytes);
-          if (!g.a_mn) {
+          if (!a_mn) {
             tma_load_2d_pair(sa, ma, full0, k0, m0);
           } else {
             tma_load_2d_pair(sa, ma, full0, m0, k0);
             tma_load_2d_pair(sa + 8192, ma, full0, m0 + 64, k0);
           }
-          if (!g.b_mn) {
+          if (!b_mn) {
             tma_load_2d_pair(sb, mb, full0, k0, n0);
           } else {
 #pragma unroll
@@ -239,11 +257,15 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
   } else if (warp == 1) {
     // ---------------- MMA issuer (rank 0 only) ----------------
     if (rank == 0 && lane == 0) {
-      const uint64_t step_a = desc_step(g.a_mn), step_b = desc_step(g.b_mn);
       int stage = 0;
       uint32_t phase = 0;
       int it = 0;
       for (int t = pair; t < n_tiles; t += n_pairs, ++it) {
+        const PairProduct& p = g.p[tile_at<CN>(g, t).product];
+        const int num_kb = p.kb[0] + p.kb[1];
+        const bool a_mn = p.a_mn, b_mn = p.b_mn;
+        const uint64_t step_a = desc_step(a_mn), step_b = desc_step(b_mn);
+        const uint32_t idesc = p.idesc;
         const int acc = it & 1;
         const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
         mbar_wait(acce_bar(acc), acc_phase ^ 1u, dead, g.err);  // both CTAs' epilogues have drained it
@@ -253,10 +275,10 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
           mbar_wait(full_bar(stage), phase, dead, g.err);
           tc_fence_after();
           const uint32_t sa = tiles + stage * C::kStageBytes;
-          const uint64_t da = smem_desc(sa, g.a_mn), db = smem_desc(sa + BM * 128, g.b_mn);
+          const uint64_t da = smem_desc(sa, a_mn), db = smem_desc(sa + BM * 128, b_mn);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            tc_mma<I8, 2>(d_tmem, da + step_a * k, db + step_b * k, g.idesc, (kb | k) != 0 ? 1u : 0u);
+            tc_mma<I8, 2>(d_tmem, da + step_a * k, db + step_b * k, idesc, (kb | k) != 0 ? 1u : 0u);
           tc_commit_pair(empty_bar(stage));                 // frees the stage in this CTA ...
           tc_commit_pair(map_to_cta(empty_bar(stage), 1));  // ... and in the peer
           if (++stage == S) {
@@ -281,20 +303,24 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
     int it = 0;
     for (int t = pair; t < n_tiles; t += n_pairs, ++it) {
       const Tile tile = tile_at<CN>(g, t);
+      const PairProduct& p = g.p[tile.product];
+      const auto& mp = maps.p[tile.product];
+      const int m = p.m, n = p.n;
+      const bool tma = p.tma_store;
       const int row0 = tile.m0 + (int)rank * BM + quarter * 32;
       const int row = row0 + lane;
       const int acc = it & 1;
       const uint32_t acc_phase = (uint32_t)(it >> 1) & 1u;
       const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN);
-      const bool rows_any = row0 < g.m;
+      const bool rows_any = row0 < m;
       float sa = 0.f;
-      if (I8 && row < g.m) sa = g.scale_a[row];
-      uint4 kept[2][6];  // GATE_GRAD: g and u of the 32 columns that come next
+      if (I8 && row < m) sa = g.scale_a[row];
+      uint4 kept[2][6];  // GATE_GRAD: the factors of the 32 columns that come next
       auto fetch_kept = [&](int col) {
-        if (rows_any && col < g.n) {
-          const uint8_t* b = g.gu + gu_block_offset(row0, col, g.gu_cols);
-          gu_fetch(b, lane, kept[0]);
-          gu_fetch(b + kGuHalf, lane, kept[1]);
+        if (rows_any && col < n) {
+          const uint8_t* b = g.kept + kept_offset(row0, col, g.kept_cols);
+          kept_fetch(b, lane, kept[0]);
+          kept_fetch(b + kKeptHalf, lane, kept[1]);
         }
       };
       if (EPI == OPS_GATE_GRAD) fetch_kept(tile.n0 + half * kMine * 64);
@@ -305,9 +331,9 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
         for (int u = 0; u < kMine; ++u) {
           const int c0 = (half * kMine + u) * 64;  // column in the tile
           const int col0 = tile.n0 + c0;
-          const bool any = rows_any && col0 < g.n;
+          const bool any = rows_any && col0 < n;
           if (EPI == OPS_STORE || EPI == OPS_GATE) {
-            if (g.tma_store) stage_free(lane);
+            if (tma) stage_free(lane);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               uint32_t w[16];
@@ -323,24 +349,42 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
                 tc_ld32(t0 + c0 + 32 * h, rg);
                 tc_ld32(t0 + CN + c0 + 32 * h, ru);
                 tc_wait_ld();
-                if (g.gu && rows_any && col < g.n) {
-                  uint8_t* b = g.gu + gu_block_offset(row0, col, g.gu_cols);
-                  gu_store(b, lane, rg);
-                  gu_store(b + kGuHalf, lane, ru);
-                }
+                if (g.kept) {
+                  // rg, ru become the factors that are kept
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  const float h0 = gate_value(__uint_as_float(rg[2 * i]), gelu) * __uint_as_float(ru[2 * i]);
-                  const float h1 = gate_value(__uint_as_float(rg[2 * i + 1]), gelu) * __uint_as_float(ru[2 * i + 1]);
-                  w[i] = pack16(h0, h1, f16);
+                  for (int i = 0; i < 16; ++i) {
+                    float h2[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                      const float v = __uint_as_float(ru[2 * i + e]);
+                      float a, da;
+                      gate_grad(__uint_as_float(rg[2 * i + e]), gelu, a, da);
+                      h2[e] = a * v;
+                      rg[2 * i + e] = __float_as_uint(v * da);
+                      ru[2 * i + e] = __float_as_uint(a);
+                    }
+                    w[i] = pack16(h2[0], h2[1], f16);
+                  }
+                  if (rows_any && col < n) {
+                    uint8_t* b = g.kept + kept_offset(row0, col, g.kept_cols);
+                    kept_store(b, lane, rg);
+                    kept_store(b + kKeptHalf, lane, ru);
+                  }
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) {
+                    const float h0 = gate_value(__uint_as_float(rg[2 * i]), gelu) * __uint_as_float(ru[2 * i]);
+                    const float h1 = gate_value(__uint_as_float(rg[2 * i + 1]), gelu) * __uint_as_float(ru[2 * i + 1]);
+                    w[i] = pack16(h0, h1, f16);
+                  }
                 }
               }
               stage_half(buf, lane, h, w);
             }
-            if (g.tma_store)
-              stage_send(&maps.c[tile.group], buf_addr, lane, col0, row0, any);
+            if (tma)
+              stage_send(&mp.c[0], buf_addr, lane, col0, row0, any);
             else
-              rows_out16(buf, g.c[tile.group], g.ldc, lane, row0, col0, g.m, g.n);
+              rows_out16(buf, p.c, p.ldc, lane, row0, col0, m, n);
           } else if (EPI == OPS_GATE_GRAD) {
             stage_free(lane);
 #pragma unroll
@@ -350,17 +394,9 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
               tc_wait_ld();
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
-                float dg[2], du[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  float a, da;
-                  gate_grad(gu_value(kept[0], 2 * i + e), gelu, a, da);
-                  const float dh = __uint_as_float(r[2 * i + e]);
-                  dg[e] = dh * gu_value(kept[1], 2 * i + e) * da;
-                  du[e] = dh * a;
-                }
-                wg[i] = pack16(dg[0], dg[1], f16);
-                wu[i] = pack16(du[0], du[1], f16);
+                const float d0 = __uint_as_float(r[2 * i]), d1 = __uint_as_float(r[2 * i + 1]);
+                wg[i] = pack16(d0 * kept_value(kept[0], 2 * i), d1 * kept_value(kept[0], 2 * i + 1), f16);
+                wu[i] = pack16(d0 * kept_value(kept[1], 2 * i), d1 * kept_value(kept[1], 2 * i + 1), f16);
               }
               if (h == 0 || u + 1 < kMine) fetch_kept(col0 + 32 * h + 32);
               stage_half(buf, lane, h, wg);
@@ -369,13 +405,13 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
             fence_async_shared();
             __syncwarp();
             if (lane == 0 && any) {
-              tma_store_2d(&maps.c[0], buf_addr, col0, row0);
-              tma_store_2d(&maps.c[1], buf_addr + kStoreBytes, col0, row0);
+              tma_store_2d(&mp.c[0], buf_addr, col0, row0);
+              tma_store_2d(&mp.c[1], buf_addr + kStoreBytes, col0, row0);
               bulk_commit();
             }
           } else {
             const bool f32 = g.out_type == ASD_TYPE_F32;
-            if (g.tma_store) stage_free(lane);
+            if (tma) stage_free(lane);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int col = col0 + 32 * h;
@@ -385,21 +421,21 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
               float f[32];
               // every lane needs the same columns' scales: one load per lane, handed around
               const int mine = col + lane;
-              const float sb = mine < g.n ? g.scale_b[mine] : 0.f;
-              const float bb = g.bias && mine < g.n ? g.bias[mine] : 0.f;
+              const float sb = mine < n ? g.scale_b[mine] : 0.f;
+              const float bb = g.bias && mine < n ? g.bias[mine] : 0.f;
 #pragma unroll
               for (int i = 0; i < 32; ++i)
                 f[i] = fmaf((float)(int)r[i] * sa, __shfl_sync(0xffffffffu, sb, i), __shfl_sync(0xffffffffu, bb, i));
               if (f32) {
-                if (g.tma_store && h == 1) stage_free(lane);
+                if (tma && h == 1) stage_free(lane);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                   stage_put(buf, lane, i, make_uint4(__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]),
                                                      __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3])));
-                if (g.tma_store)
-                  stage_send(&maps.c[0], buf_addr, lane, col, row0, rows_any && col < g.n);
+                if (tma)
+                  stage_send(&mp.c[0], buf_addr, lane, col, row0, rows_any && col < n);
                 else
-                  rows_out32(buf, g.c[0], g.ldc, lane, row0, col, g.m, g.n);
+                  rows_out32(buf, p.c, p.ldc, lane, row0, col, m, n);
               } else {
                 uint32_t w[16];
 #pragma unroll
@@ -408,10 +444,10 @@ op_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ Pa
               }
             }
             if (!f32) {
-              if (g.tma_store)
-                stage_send(&maps.c[0], buf_addr, lane, col0, row0, any);
+              if (tma)
+                stage_send(&mp.c[0], buf_addr, lane, col0, row0, any);
               else
-                rows_out16(buf, g.c[0], g.ldc, lane, row0, col0, g.m, g.n);
+                rows_out16(buf, p.c, p.ldc, lane, row0, col0, m, n);
             }
           }
         }
@@ -461,65 +497,87 @@ bool encode_operand(CUtensorMap* out, const Operand& x, int type, bool i8, int t
 namespace {
 
 template <int BN, int EPI>
-asd_status launch_pair(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
+asd_status launch_pair(const asd_ops* o, const OpsGemm* list, int count, cudaStream_t st) {
   using C = OpPairCfg<BN, EPI>;
   constexpr bool I8 = EPI == OPS_I8;
-  constexpr int CN = EPI == OPS_GATE ? BN / 2 : BN;
-  PairMaps maps;
+  constexpr int CN = EPI == OPS_GATE ? BN / 2 : BN, N = products_of<EPI>;
+  PairMaps<N> maps;
   memset(&maps, 0, sizeof(maps));
-  PairArgs g{};
+  PairArgs<N> g{};
   const int ke = I8 ? 128 : 64;
-  g.m = (int)q.m, g.n = (int)q.n;
-  g.kb[0] = (int)((q.k[0] + ke - 1) / ke);
-  g.kb[1] = q.parts == 2 ? (int)((q.k[1] + ke - 1) / ke) : 0;
-  g.groups = q.groups;
-  g.tiles_m = (int)((q.m + 2 * BM - 1) / (2 * BM));
-  g.tiles_n = (int)((q.n + CN - 1) / CN);
-  g.a_mn = q.a[0].mn, g.b_mn = q.b[0].mn;
-  const uint32_t fmt = I8 ? 1u : (q.type == ASD_TYPE_BF16 ? 1u : 0u);  // signed 8-bit; bf16 or fp16
-  g.idesc = (I8 ? 2u << 4 : 1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)g.a_mn << 15) | ((uint32_t)g.b_mn << 16) |
-            ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((2 * BM) >> 4) << 24);
+  int64_t tiles = 0;
+  for (int j = 0; j < N; ++j) {
+    PairProduct& p = g.p[j];
+    p.first = INT_MAX;
+    if (j >= count) continue;
+    const OpsGemm& q = list[j];
+    p.m = (int)q.m, p.n = (int)q.n;
+    p.kb[0] = (int)((q.k[0] + ke - 1) / ke);
+    p.kb[1] = q.parts == 2 ? (int)((q.k[1] + ke - 1) / ke) : 0;
+    p.tiles_m = (int)((q.m + 2 * BM - 1) / (2 * BM));
+    p.tiles_n = (int)((q.n + CN - 1) / CN);
+    p.first = (int)tiles;
+    tiles += (int64_t)p.tiles_m * p.tiles_n;
+    p.a_mn = q.a[0].mn, p.b_mn = q.b[0].mn;
+    const uint32_t fmt = I8 ? 1u : (q.type == ASD_TYPE_BF16 ? 1u : 0u);  // signed 8-bit; bf16 or fp16
+    p.idesc = (I8 ? 2u << 4 : 1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
+              ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((2 * BM) >> 4) << 24);
+    p.c = q.c[0];
+    p.ldc = q.ldc;
+    const int es = ops_type_size(q.type), outs = EPI == OPS_GATE_GRAD ? 2 : 1;
+    p.tma_store = 1;
+    for (int i = 0; i < outs; ++i)
+      if (((uintptr_t)q.c[i] & 15) || (q.ldc * es) % 16) p.tma_store = 0;
+    bool ok = true;
+    for (int i = 0; i < 2; ++i) {
+      ok = ok && encode_operand(&maps.p[j].a[i], q.a[q.parts == 2 ? i : 0], q.type, I8, BM);
+      ok = ok && encode_operand(&maps.p[j].b[i], q.b[q.parts == 2 || EPI == OPS_GATE ? i : 0], q.type, I8, BN / 2);
+      if (p.tma_store) ok = ok && encode(&maps.p[j].c[i], map_type(q.type), es, q.c[i < outs ? i : 0], q.m, q.n, q.ldc, 32);
+    }
+    if (!ok) return ops_fail(ASD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+  }
+  const OpsGemm& q = list[0];
+  g.tiles = (int)tiles;
   g.out_type = q.type;
   g.gelu = q.act == ASD_ACT_GELU;
-  g.ldc = q.ldc;
-  g.gu = q.gu;
-  g.gu_cols = (int)((q.n + 31) / 32);
+  g.kept = q.kept;
+  g.kept_cols = (int)((q.n + 31) / 32);
   g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias;
   g.err = o->err;
-  const bool two_b = q.parts == 2 || q.groups == 2 || EPI == OPS_GATE;
-  const int es = ops_type_size(q.type);
-  const int outs = q.groups == 2 || EPI == OPS_GATE_GRAD ? 2 : 1;
-  g.tma_store = 1;
-  for (int i = 0; i < outs; ++i) {
-    g.c[i] = q.c[i];
-    if (((uintptr_t)q.c[i] & 15) || (q.ldc * es) % 16) g.tma_store = 0;
-  }
-  bool ok = true;
-  for (int i = 0; i < 2; ++i) {
-    ok = ok && encode_operand(&maps.a[i], q.a[q.parts == 2 || q.groups == 2 ? i : 0], q.type, I8, BM);
-    ok = ok && encode_operand(&maps.b[i], q.b[two_b ? i : 0], q.type, I8, BN / 2);
-    if (g.tma_store) ok = ok && encode(&maps.c[i], map_type(q.type), es, q.c[i < outs ? i : 0], q.m, q.n, q.ldc, 32);
-  }
-  if (!ok) return ops_fail(ASD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-  const int64_t n_tiles = (int64_t)g.groups * g.tiles_m * g.tiles_n;
-  const int pairs = (int)std::min<int64_t>(n_tiles, o->num_sms / 2);
+  const int pairs = (int)std::min<int64_t>(tiles, o->num_sms / 2);
   ops_launch(op_pair_kernel<BN, EPI>, dim3(2 * pairs), dim3(kPairThreads), (size_t)C::kSmemBytes, st, 1, maps, g);
   return ops_launched("matrix product");
 }
 
-// Clocks of a launch with tiles of width bn: waves of tiles, of which one costs the larger of its MMAs' time and its
-// operands' way into shared memory (a k-block of 128 bytes: 2 bn clocks, 128 (128 + bn / 2) bytes at some 50 bytes a
-// clock); some 5000 to start, drain the last tile and end.
-double pair_clocks(const asd_ops* o, const OpsGemm& q, int bn) {
-  const int cn = q.epi == OPS_GATE ? bn / 2 : bn, ke = q.epi == OPS_I8 ? 128 : 64;
-  const int64_t kb = (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
-  const int64_t tiles = (int64_t)q.groups * ((q.m + 2 * BM - 1) / (2 * BM)) * ((q.n + cn - 1) / cn);
-  const int64_t waves = (tiles + o->num_sms / 2 - 1) / (o->num_sms / 2);
-  return (double)(waves * kb) * std::max(2.0 * bn, (BM + bn / 2) * 128 / 50.0) + 5000.0;
+// Clocks of a k-block (128 bytes of k) of a tile of width bn: the larger of its MMAs' time, 2 bn, and its operands' way
+// into shared memory, 128 (128 + bn / 2) bytes at some 50 bytes a clock.
+double kblock_clocks(int bn) { return std::max(2.0 * bn, (BM + bn / 2) * 128 / 50.0); }
+int64_t pair_tiles(const OpsGemm& q, int bn) {
+  const int cn = q.epi == OPS_GATE ? bn / 2 : bn;
+  return ((q.m + 2 * BM - 1) / (2 * BM)) * ((q.n + cn - 1) / cn);
+}
+int64_t pair_kblocks(const OpsGemm& q) {
+  const int ke = q.epi == OPS_I8 ? 128 : 64;
+  return (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
+}
+// Clocks of a launch: the tiles go to the clusters in turn, and the longest row of them counts; some 5000 to start, drain
+// the last tile and end.
+double list_clocks(const asd_ops* o, const OpsGemm* list, int count, int bn) {
+  const int units = o->num_sms / 2;
+  double load[256] = {};
+  int64_t first = 0;
+  for (int j = 0; j < count; ++j) {
+    const int64_t tiles = pair_tiles(list[j], bn), each = tiles / units;
+    const double t = pair_kblocks(list[j]) * kblock_clocks(bn);
+    for (int u = 0; u < units; ++u) load[u] += t * (each + ((u - first % units + units) % units < tiles % units ? 1 : 0));
+    first += tiles;
+  }
+  return *std::max_element(load, load + units) + 5000.0;
 }
 template <int EPI>
-asd_status launch_width(const asd_ops* o, const OpsGemm& q, cudaStream_t st) {
-  return pair_clocks(o, q, 256) <= pair_clocks(o, q, 128) ? launch_pair<256, EPI>(o, q, st) : launch_pair<128, EPI>(o, q, st);
+asd_status launch_width(const asd_ops* o, const OpsGemm* list, int count, cudaStream_t st) {
+  return list_clocks(o, list, count, 256) <= list_clocks(o, list, count, 128) ? launch_pair<256, EPI>(o, list, count, st)
+                                                                             : launch_pair<128, EPI>(o, list, count, st);
 }
 
 template <int BN, int EPI>
@@ -529,20 +587,40 @@ cudaError_t prepare_pair() {
 
 }  // namespace
 
-int64_t gated_saved_gu_bytes(int64_t rows, int64_t hidden) { return (rows + 31) / 32 * ((hidden + 31) / 32) * kGuBlock; }
+int64_t gated_kept_bytes(int64_t rows, int64_t hidden) { return (rows + 31) / 32 * ((hidden + 31) / 32) * kKeptBlock; }
+
+namespace {
+// Whether a product is better split than tiled; `plan` is how.
+bool better_split(const asd_ops* o, const OpsGemm& q, SplitPlan* plan) {
+  if (q.a[0].mn) return false;
+  *plan = plan_split(o, q);
+  return plan->clocks < std::min(list_clocks(o, &q, 1, 256), list_clocks(o, &q, 1, 128));
+}
+}  // namespace
 
 asd_status ops_gemm(const asd_ops* o, const OpsGemm& q, bool early, cudaStream_t st) {
   if (use_stream(q)) return ops_gemm_stream(o, q, early, st);
-  if (q.groups == 1 && !q.a[0].mn) {
-    const SplitPlan p = plan_split(o, q);
-    if (p.clocks < std::min(pair_clocks(o, q, 256), pair_clocks(o, q, 128))) return ops_gemm_split(o, q, p, early, st);
-  }
+  SplitPlan p;
+  if (better_split(o, q, &p)) return ops_gemm_split(o, q, p, early, st);
   switch (q.epi) {
-    case OPS_STORE: return launch_width<OPS_STORE>(o, q, st);
-    case OPS_GATE: return launch_width<OPS_GATE>(o, q, st);
-    case OPS_GATE_GRAD: return launch_width<OPS_GATE_GRAD>(o, q, st);
-    default: return launch_width<OPS_I8>(o, q, st);
+    case OPS_STORE: return launch_width<OPS_STORE>(o, &q, 1, st);
+    case OPS_GATE: return launch_width<OPS_GATE>(o, &q, 1, st);
+    case OPS_GATE_GRAD: return launch_width<OPS_GATE_GRAD>(o, &q, 1, st);
+    default: return launch_width<OPS_I8>(o, &q, 1, st);
   }
+}
+
+// One launch of tiles for all of the list, so that the last, partly filled wave of tiles comes once and not once for each
+// product.  A first product (the one with the longest sum) that is better split goes by itself; whether it is does not
+// depend on the others, so that a gradient has the same bits whichever are asked for.
+asd_status ops_gemm_list(const asd_ops* o, const OpsGemm* list, int count, cudaStream_t st) {
+  SplitPlan p;
+  if (count && better_split(o, list[0], &p)) {
+    const asd_status s = ops_gemm_split(o, list[0], p, false, st);
+    if (s != ASD_OK) return s;
+    ++list, --count;
+  }
+  return count ? launch_width<OPS_STORE>(o, list, count, st) : ASD_OK;
 }
 
 asd_status ops_gemm_prepare() {

@@ -57,11 +57,19 @@ struct Mat {
 inline bool mat_aligned(const Mat& m) { return ((uintptr_t)m.p & 15) == 0 && (m.ld * m.es) % 16 == 0; }
 
 // ---- asd_ops_rows.cu: one row at a time -------------------------------------------------------------
+asd_status ops_rows_prepare();
 void launch_rmsnorm(const asd_ops* o, const asd_rmsnorm_args* a, cudaStream_t st);
 int64_t rmsnorm_backward_bytes(const asd_ops* o, const asd_rmsnorm_backward_args* a);
 void launch_rmsnorm_backward(const asd_ops* o, const asd_rmsnorm_backward_args* a, cudaStream_t st);
 void launch_quantize(const asd_ops* o, const asd_quantize_args* a, cudaStream_t st);
-void launch_pack(const asd_ops* o, const Mat& src, void* dst, int64_t ld_dst, cudaStream_t st);
+// Operands that are copied to rows of a multiple of 16 bytes before a product reads them, in one launch.
+struct Packs {
+  int n = 0;
+  Mat src[4];
+  void* dst[4];
+  int64_t ld[4];  // elements
+};
+void launch_packs(const asd_ops* o, const Packs& packs, cudaStream_t st);
 
 // ---- asd_ops_gemm.cu: matrix products -----------------------------------------------------------------
 // C[m, n] = sum_k A(m, k) B(n, k).  An operand is read either as a row-major matrix [its m or n, k] or, `mn` true, as
@@ -74,21 +82,23 @@ enum OpsEpi { OPS_STORE = 0, OPS_GATE = 1, OPS_GATE_GRAD = 2, OPS_I8 = 3 };
 struct OpsGemm {
   int epi;
   int type;    // asd_type of the 16-bit operands and outputs (OPS_I8: of the output)
-  int act;     // OPS_GATE, OPS_GATE_GRAD
+  int act;     // OPS_GATE
   int64_t m, n, k[2];
   int parts;   // OPS_STORE: 1, or 2 sums over k one after the other (k[0] of a[0], b[0], then k[1] of a[1], b[1])
-  int groups;  // OPS_STORE: 1, or 2 products side by side (a[g], b[g] -> c[g])
   Operand a[2], b[2];  // OPS_GATE: b[0] the gate's weights, b[1] the value's
   void* c[2];          // outputs; OPS_GATE: c[0] = h; OPS_GATE_GRAD: c[0] = dg, c[1] = du
   int64_t ldc;
-  uint8_t* gu;         // OPS_GATE: where g and u are kept, or NULL; OPS_GATE_GRAD: where they were
+  uint8_t* kept;       // OPS_GATE: where the gate's two factors are kept, or NULL; OPS_GATE_GRAD: where they were
   const float* scale_a;  // OPS_I8
   const float* scale_b;
   const float* bias;
 };
-int64_t gated_saved_gu_bytes(int64_t rows, int64_t hidden);
+int64_t gated_kept_bytes(int64_t rows, int64_t hidden);
 // `early`: the kernel before this one in the stream belongs to the same call, which does not write b.
 asd_status ops_gemm(const asd_ops* o, const OpsGemm& g, bool early, cudaStream_t st);
+// Up to four independent OPS_STORE products of one type.
+constexpr int kMostProducts = 4;
+asd_status ops_gemm_list(const asd_ops* o, const OpsGemm* g, int n, cudaStream_t st);
 asd_status ops_gemm_prepare();  // per device: opt-in to large shared memory
 
 // ---- asd_ops_stream.cu: matrix products of few rows ---------------------------------------------------

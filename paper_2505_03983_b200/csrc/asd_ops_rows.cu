@@ -290,22 +290,95 @@ __global__ void __launch_bounds__(block_of<TPR>) rmsnorm_kernel(const NormArgs a
 }
 
 struct QuantArgs {
-  int rows, width, act;
+  int rows, width, act, stride;  // stride: rows that are worked on side by side
   const void* x;
   int8_t* q;
   float* scale;
   int64_t ld_x, ld_q;
 };
 
-template <typename T, int VEC, int TPR, bool LONG>
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A row's threads walk over rows.  With the gate, 16-bit rows that can be read in 16-byte pieces come through shared memory
+// one row ahead (cp.async; a thread reads back only what it has copied itself, so that takes no barrier): two transcendental
+// instructions an element and the barrier of the row's maximum would leave memory idle otherwise.
+template <typename T, int VEC>
+constexpr bool row_ahead = VEC == 8 && sizeof(T) == 2;
+template <typename T, int VEC, int TPR>
+constexpr int quantize_smem = row_ahead<T, VEC> ? 2 * 2 * kPer * 2 * block_of<TPR> : 0;
+
+template <typename T, int VEC, int TPR>
 __global__ void __launch_bounds__(block_of<TPR>) quantize_kernel(const QuantArgs a) {
   constexpr int NV = kPer / VEC;
-  __shared__ uint32_t buf_m[TPR / 32];
+  constexpr bool AHEAD = row_ahead<T, VEC>;
+  extern __shared__ __align__(16) uint4 ahead[];  // [2 rows][g, u][NV][threads]
+  __shared__ uint32_t buf_m[2][TPR / 32];
   dep_wait();
   dep_launch();
   const int t = TPR == 32 ? (threadIdx.x & 31) : threadIdx.x;
-  const int row = TPR == 32 ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
-  if (row >= a.rows) return;
+  const int first = TPR == 32 ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+  const bool gate = a.act != ASD_ACT_NONE;
+  auto slot = [&](int turn, int part, int v) { return ahead + ((turn * 2 + part) * NV + v) * block_of<TPR> + threadIdx.x; };
+  auto fetch = [&](int64_t row, int turn) {
+    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ld_x;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) {
+        copy_16((uint32_t)__cvta_generic_to_shared(slot(turn, 0, v)), x + col);
+        if (gate) copy_16((uint32_t)__cvta_generic_to_shared(slot(turn, 1, v)), x + a.width + col);
+      }
+    }
+  };
+  if (AHEAD) {
+    if (first < a.rows) fetch(first, 0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  int turn = 0;
+  for (int64_t row = first; row < a.rows; row += a.stride, turn ^= 1) {
+    if (AHEAD) {
+      if (row + a.stride < a.rows) fetch(row + a.stride, turn ^ 1);
+      asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
+    }
+    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ld_x;
+    float f[NV][VEC];
+    uint32_t most = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) {
+        load_vec<VEC, T>(AHEAD ? reinterpret_cast<const T*>(slot(turn, 0, v)) : x + col, f[v]);
+        if (gate) {
+          float u[VEC];
+          load_vec<VEC, T>(AHEAD ? reinterpret_cast<const T*>(slot(turn, 1, v)) : x + a.width + col, u);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) f[v][i] = act_value(f[v][i], a.act) * u[i];
+        }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) most = max(most, mag(f[v][i]));
+      }
+    }
+    const RowScale rs = row_scale(row_max<TPR>(most, buf_m[turn]));
+    int8_t* q = a.q + row * a.ld_q;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * TPR + t) * VEC;
+      if (col < a.width) put_q<VEC>(q + col, f[v], rs);
+    }
+    if (t == 0) a.scale[row] = rs.scale;
+  }
+}
+
+// Rows of more than 16384, read twice.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(512) quantize_long_kernel(const QuantArgs a) {
+  __shared__ uint32_t buf_m[16];
+  dep_wait();
+  dep_launch();
+  const int t = threadIdx.x;
+  const int64_t row = blockIdx.x;
   const T* x = reinterpret_cast<const T*>(a.x) + row * a.ld_x;
   int8_t* q = a.q + row * a.ld_q;
   auto fetch = [&](int col, float(&f)[VEC]) {
@@ -318,39 +391,19 @@ __global__ void __launch_bounds__(block_of<TPR>) quantize_kernel(const QuantArgs
     }
   };
   uint32_t most = 0;
-  if constexpr (!LONG) {
-    float f[NV][VEC];
+  for (int col = t * VEC; col < a.width; col += 512 * VEC) {
+    float f[VEC];
+    fetch(col, f);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * TPR + t) * VEC;
-      if (col < a.width) {
-        fetch(col, f[v]);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) most = max(most, mag(f[v][i]));
-      }
-    }
-    const RowScale rs = row_scale(row_max<TPR>(most, buf_m));
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * TPR + t) * VEC;
-      if (col < a.width) put_q<VEC>(q + col, f[v], rs);
-    }
-    if (t == 0) a.scale[row] = rs.scale;
-  } else {
-    for (int col = t * VEC; col < a.width; col += TPR * VEC) {
-      float f[VEC];
-      fetch(col, f);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) most = max(most, mag(f[i]));
-    }
-    const RowScale rs = row_scale(row_max<TPR>(most, buf_m));
-    for (int col = t * VEC; col < a.width; col += TPR * VEC) {
-      float f[VEC];
-      fetch(col, f);
-      put_q<VEC>(q + col, f, rs);
-    }
-    if (t == 0) a.scale[row] = rs.scale;
+    for (int i = 0; i < VEC; ++i) most = max(most, mag(f[i]));
   }
+  const RowScale rs = row_scale(row_max<512>(most, buf_m));
+  for (int col = t * VEC; col < a.width; col += 512 * VEC) {
+    float f[VEC];
+    fetch(col, f);
+    put_q<VEC>(q + col, f, rs);
+  }
+  if (t == 0) a.scale[row] = rs.scale;
 }
 
 struct NormGradArgs {
@@ -549,14 +602,48 @@ __global__ void __launch_bounds__(1024) reduce_dw_kernel(const float* part, int 
   if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < width) dw[blockIdx.x * 32 + threadIdx.y] = from_f<W>(v);
 }
 
-// Rows of `cols` elements, ld_src apart, to rows ld_dst apart.
-template <typename E>
-__global__ void __launch_bounds__(256) pack_rows_kernel(const E* src, int64_t ld_src, int64_t rows, int cols, E* dst, int64_t ld_dst) {
+// Up to four matrices to rows of a multiple of 16 bytes, in one launch (blockIdx.y).  A thread makes 16 bytes of a row from
+// the aligned words that hold them, each shifted by the row's misalignment; a row's last bytes, and elements of a row that
+// does not start on a word, are read one by one where a word would reach outside the row.
+constexpr int kMostPacks = 4;
+struct PackArgs {
+  struct One {
+    const uint8_t* src;
+    uint8_t* dst;
+    int64_t rows, ld_src, ld_dst;  // bytes
+    int bytes;                     // of a row
+  } m[kMostPacks];
+};
+__global__ void __launch_bounds__(256) pack_rows_kernel(const PackArgs a) {
   dep_wait();
   dep_launch();
-  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y)
-    for (int col = blockIdx.x * 256 + threadIdx.x; col < cols; col += gridDim.x * 256)
-      dst[row * ld_dst + col] = src[row * ld_src + col];
+  const PackArgs::One m = a.m[blockIdx.y];
+  const int pieces = (m.bytes + 15) / 16;
+  const int64_t total = m.rows * pieces;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / pieces;
+    const int at = (int)(i - row * pieces) * 16;
+    const uint8_t* p = m.src + row * m.ld_src + at;
+    const int off = (int)((uintptr_t)p & 3);
+    uint32_t w[4];
+    if (at >= off && at + 20 <= m.bytes) {  // the five words around the piece lie inside the row
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(p - off);
+      uint32_t v[5];
+#pragma unroll
+      for (int k = 0; k < 5; ++k) v[k] = q[k];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(v[k], v[k + 1], 8 * off);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[k] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at + 4 * k + e < m.bytes) w[k] |= (uint32_t)p[4 * k + e] << (8 * e);
+      }
+    }
+    *reinterpret_cast<uint4*>(m.dst + row * m.ld_dst + at) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
 }
 
 bool aligned(const void* p, int64_t ld, int es, int bytes) { return ((uintptr_t)p % bytes) == 0 && (ld * es) % bytes == 0; }
@@ -592,19 +679,28 @@ void rmsnorm_type(const asd_ops* o, const NormArgs& n, bool vec, bool q8, cudaSt
     q8 ? rmsnorm_t<T, 1, true>(o, n, st) : rmsnorm_t<T, 1, false>(o, n, st);
 }
 
+template <typename T, int VEC, int TPR>
+void quantize_rows(const asd_ops* o, QuantArgs n, cudaStream_t st) {
+  const int per_block = TPR == 32 ? 4 : 1;
+  constexpr int smem = quantize_smem<T, VEC, TPR>;
+  // as many blocks as the SMs hold together
+  const int blocks = (n.rows + per_block - 1) / per_block, most = o->num_sms * (smem ? 232448 / (smem + 1024) : 1024 / block_of<TPR>);
+  const int grid = blocks < most ? blocks : most;
+  n.stride = grid * per_block;
+  ops_launch(quantize_kernel<T, VEC, TPR>, dim3(grid), dim3(block_of<TPR>), (size_t)smem, st, 1, n);
+}
 template <typename T, int VEC>
 void quantize_t(const asd_ops* o, const QuantArgs& n, cudaStream_t st) {
-  const int tpr = row_threads(o, n.rows, n.width);
-  if (tpr == 32)
-    ops_launch(quantize_kernel<T, VEC, 32, false>, dim3((n.rows + 3) / 4), dim3(128), 0, st, 1, n);
-  else if (tpr == 128)
-    ops_launch(quantize_kernel<T, VEC, 128, false>, dim3(n.rows), dim3(128), 0, st, 1, n);
-  else if (tpr == 256)
-    ops_launch(quantize_kernel<T, VEC, 256, false>, dim3(n.rows), dim3(256), 0, st, 1, n);
-  else if (n.width <= 512 * kPer)
-    ops_launch(quantize_kernel<T, VEC, 512, false>, dim3(n.rows), dim3(512), 0, st, 1, n);
-  else
-    ops_launch(quantize_kernel<T, VEC, 512, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
+  if (n.width > 512 * kPer) {
+    ops_launch(quantize_long_kernel<T, VEC>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    return;
+  }
+  switch (row_threads(o, n.rows, n.width)) {
+    case 32: return quantize_rows<T, VEC, 32>(o, n, st);
+    case 128: return quantize_rows<T, VEC, 128>(o, n, st);
+    case 256: return quantize_rows<T, VEC, 256>(o, n, st);
+    default: return quantize_rows<T, VEC, 512>(o, n, st);
+  }
 }
 
 constexpr int kGradWidth = 8192;  // the longest row whose sums of dw a block keeps in registers
@@ -661,6 +757,19 @@ void launch_quantize(const asd_ops* o, const asd_quantize_args* a, cudaStream_t 
     vec ? quantize_t<__nv_bfloat16, 8>(o, n, st) : quantize_t<__nv_bfloat16, 1>(o, n, st);
 }
 
+namespace {
+template <typename T>
+cudaError_t prepare_quantize() {
+  const cudaError_t e = cudaFuncSetAttribute(quantize_kernel<T, 8, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize, quantize_smem<T, 8, 256>);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(quantize_kernel<T, 8, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, quantize_smem<T, 8, 512>);
+}
+}  // namespace
+asd_status ops_rows_prepare() {
+  for (cudaError_t e : {prepare_quantize<__half>(), prepare_quantize<__nv_bfloat16>()})
+    if (e != cudaSuccess) return ops_fail(ASD_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+  return ASD_OK;
+}
+
 int64_t rmsnorm_backward_bytes(const asd_ops* o, const asd_rmsnorm_backward_args* a) {
   if (!a->dw || a->rows == 0) return 0;
   return 4 * ((int64_t)grad_blocks(o, a->rows, a->width) * a->width + (a->width > kGradWidth ? a->rows : 0));
@@ -697,16 +806,19 @@ void launch_rmsnorm_backward(const asd_ops* o, const asd_rmsnorm_backward_args* 
                reinterpret_cast<__nv_bfloat16*>(a->dw));
 }
 
-void launch_pack(const asd_ops* o, const Mat& src, void* dst, int64_t ld_dst, cudaStream_t st) {
-  const int bx = (int)((src.cols + 255) / 256 < 64 ? (src.cols + 255) / 256 : 64);
-  int64_t by = (int64_t)o->num_sms * 16 / bx;
-  if (by > src.rows) by = src.rows;
-  if (by < 1) by = 1;
-  const dim3 grid(bx, (unsigned)by);
-  if (src.es == 1)
-    ops_launch(pack_rows_kernel<uint8_t>, grid, dim3(256), 0, st, 1, (const uint8_t*)src.p, src.ld, src.rows, (int)src.cols, (uint8_t*)dst, ld_dst);
-  else
-    ops_launch(pack_rows_kernel<uint16_t>, grid, dim3(256), 0, st, 1, (const uint16_t*)src.p, src.ld, src.rows, (int)src.cols, (uint16_t*)dst, ld_dst);
+void launch_packs(const asd_ops* o, const Packs& packs, cudaStream_t st) {
+  if (!packs.n) return;
+  PackArgs a{};
+  int64_t most = 0;
+  for (int i = 0; i < packs.n; ++i) {
+    const Mat& s = packs.src[i];
+    const int bytes = (int)(s.cols * s.es);
+    a.m[i] = {(const uint8_t*)s.p, (uint8_t*)packs.dst[i], s.rows, s.ld * s.es, packs.ld[i] * s.es, bytes};
+    const int64_t blocks = (s.rows * ((bytes + 15) / 16) + 255) / 256;
+    most = blocks > most ? blocks : most;
+  }
+  if (most > o->num_sms * 8) most = o->num_sms * 8;
+  ops_launch(pack_rows_kernel, dim3((unsigned)most, packs.n), dim3(256), 0, st, 1, a);
 }
 
 }  // namespace asd

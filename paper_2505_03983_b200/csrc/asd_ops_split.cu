@@ -33,8 +33,8 @@ struct SplitArgs {
   int out_type, gelu;
   void* c[2];
   int64_t ldc;
-  uint8_t* gu;
-  int gu_cols;
+  uint8_t* kept;
+  int kept_cols;
   const float* scale_a;
   const float* scale_b;
   const float* bias;
@@ -225,18 +225,18 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
             reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(y, f16);
           } else if (EPI == OPS_GATE) {
             const float w = __uint_as_float(u[i]);
-            if (g.gu) {
-              uint8_t* b = g.gu + gu_block_offset(row, col, g.gu_cols);
-              gu_put(b, row & 31, col & 31, y);
-              gu_put(b + kGuHalf, row & 31, col & 31, w);
-            }
-            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(gate_value(y, gelu) * w, f16);
-          } else if (EPI == OPS_GATE_GRAD) {
-            const uint8_t* b = g.gu + gu_block_offset(row, col, g.gu_cols);
             float a, da;
-            gate_grad(gu_get(b, row & 31, col & 31), gelu, a, da);
-            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(y * gu_get(b + kGuHalf, row & 31, col & 31) * da, f16);
-            reinterpret_cast<uint16_t*>(g.c[1])[at] = round16(y * a, f16);
+            gate_grad(y, gelu, a, da);
+            if (g.kept) {
+              uint8_t* b = g.kept + kept_offset(row, col, g.kept_cols);
+              kept_put(b, row & 31, col & 31, w * da);
+              kept_put(b + kKeptHalf, row & 31, col & 31, a);
+            }
+            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(a * w, f16);
+          } else if (EPI == OPS_GATE_GRAD) {
+            const uint8_t* b = g.kept + kept_offset(row, col, g.kept_cols);
+            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(y * kept_get(b, row & 31, col & 31), f16);
+            reinterpret_cast<uint16_t*>(g.c[1])[at] = round16(y * kept_get(b + kKeptHalf, row & 31, col & 31), f16);
           } else {
             const float z = fmaf((float)(int)v[i] * g.scale_a[row], sb, bb);
             if (g.out_type == ASD_TYPE_F32)
@@ -288,7 +288,7 @@ asd_status launch_split(const asd_ops* o, const OpsGemm& q, const SplitPlan& p, 
             ((uint32_t)(BM >> 4) << 24);
   g.out_type = q.type, g.gelu = q.act == ASD_ACT_GELU;
   g.c[0] = q.c[0], g.c[1] = q.c[1], g.ldc = q.ldc;
-  g.gu = q.gu, g.gu_cols = (int)((q.n + 31) / 32);
+  g.kept = q.kept, g.kept_cols = (int)((q.n + 31) / 32);
   g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias;
   g.err = o->err;
   bool ok = true;

@@ -29,8 +29,8 @@ struct StreamArgs {
   int out_type, gelu;
   void* c;
   int64_t ldc;
-  uint8_t* gu;
-  int gu_cols;
+  uint8_t* kept;
+  int kept_cols;
   const float* scale_a;
   const float* scale_b;
   const float* bias;
@@ -168,12 +168,14 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
         if (EPI == OPS_GATE) u += __uint_as_float(p[w][row][f + 8]);
       }
       if (EPI == OPS_GATE) {
-        if (a.gu) {
-          uint8_t* b = a.gu + gu_block_offset(row, col, a.gu_cols);
-          gu_put(b, row, col & 31, v);
-          gu_put(b + kGuHalf, row, col & 31, u);
+        float act, slope;
+        gate_grad(v, a.gelu != 0, act, slope);
+        if (a.kept) {
+          uint8_t* b = a.kept + kept_offset(row, col, a.kept_cols);
+          kept_put(b, row, col & 31, u * slope);
+          kept_put(b + kKeptHalf, row, col & 31, act);
         }
-        v = gate_value(v, a.gelu != 0) * u;
+        v = act * u;
       }
       reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(v, KIND == KIND_F16);
     }
@@ -208,7 +210,7 @@ int x_pitch(int64_t k_bytes) { return (int)((k_bytes + 127) / 128 * 128 + 64); }
 // Few enough rows, and x fits into shared memory.
 bool use_stream(const OpsGemm& q) {
   const int es = q.epi == OPS_I8 ? 1 : 2;
-  return (q.epi == OPS_GATE || q.epi == OPS_I8 || (q.epi == OPS_STORE && q.parts == 1 && q.groups == 1)) && q.m <= kStreamMaxRows &&
+  return (q.epi == OPS_GATE || q.epi == OPS_I8 || (q.epi == OPS_STORE && q.parts == 1)) && q.m <= kStreamMaxRows &&
          !q.a[0].mn && !q.b[0].mn && q.m * x_pitch(q.k[0] * es) <= kStreamSmem - ring_bytes(4);
 }
 
@@ -223,7 +225,7 @@ asd_status ops_gemm_stream(const asd_ops* o, const OpsGemm& q, bool early, cudaS
   a.early = early;
   a.out_type = q.type, a.gelu = q.act == ASD_ACT_GELU;
   a.c = q.c[0], a.ldc = q.ldc;
-  a.gu = q.gu, a.gu_cols = (int)((q.n + 31) / 32);
+  a.kept = q.kept, a.kept_cols = (int)((q.n + 31) / 32);
   a.scale_a = q.scale_a, a.scale_b = q.scale_b, a.bias = q.bias;
   if (q.epi == OPS_I8)
     launch_stream<KIND_I8, OPS_I8>(o, a, st);

@@ -77,15 +77,16 @@ __device__ __forceinline__ void gate_grad(float g, bool gelu, float& a, float& d
   }
 }
 
-// g and u between the forward and the backward pass.  Rounding them to bf16 would make the gradients' error half as
-// large again as the roundings of dg, du and the result make it; fp32 would double the traffic.  Kept are the upper 24
-// bits of the fp32 value (truncated: sign, exponent and 15 bits, an error below 2^-15), the upper 16 and the next 8 in
-// separate vectors.  The order is that of the accumulator tiles, where a thread holds 32 neighbouring columns of a row:
-// a block is 32 rows x 32 columns of g, then of u, each as 4 + 2 vectors of 16 bytes for every row, vector by vector, so
-// that a warp's stores and loads are whole 512-byte runs.
-constexpr int kGuHalf = 32 * 32 * 3;
-constexpr int kGuBlock = 2 * kGuHalf;
-__device__ __forceinline__ void gu_store(uint8_t* block, int lane, const uint32_t (&v)[32]) {
+// What a training step keeps of the gate.  h = act(g) u has the derivatives act(g) in u and u act'(g) in g, and it is these
+// two factors that are kept: the backward pass then multiplies dh by them, without an exponential.  Rounding them to bf16
+// would make the gradients' error half as large again as the roundings of dg, du and the result make it; fp32 would double
+// the traffic.  Kept are the upper 24 bits of the fp32 value (truncated: sign, exponent and 15 bits, an error below 2^-15),
+// the upper 16 and the next 8 in separate vectors.  The order is that of the accumulator tiles, where a thread holds 32
+// neighbouring columns of a row: a block is 32 rows x 32 columns of u act'(g), then of act(g), each as 4 + 2 vectors of 16
+// bytes for every row, vector by vector, so that a warp's stores and loads are whole 512-byte runs.
+constexpr int kKeptHalf = 32 * 32 * 3;
+constexpr int kKeptBlock = 2 * kKeptHalf;
+__device__ __forceinline__ void kept_store(uint8_t* block, int lane, const uint32_t (&v)[32]) {
   uint4* p = reinterpret_cast<uint4*>(block) + lane;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -107,13 +108,13 @@ __device__ __forceinline__ void gu_store(uint8_t* block, int lane, const uint32_
     p[32 * (4 + i)] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
-__device__ __forceinline__ void gu_fetch(const uint8_t* block, int lane, uint4 (&r)[6]) {
+__device__ __forceinline__ void kept_fetch(const uint8_t* block, int lane, uint4 (&r)[6]) {
   const uint4* p = reinterpret_cast<const uint4*>(block) + lane;
 #pragma unroll
   for (int i = 0; i < 6; ++i) r[i] = p[32 * i];
 }
 // Column c (0..31) of a row's six vectors.
-__device__ __forceinline__ float gu_value(const uint4 (&r)[6], int c) {
+__device__ __forceinline__ float kept_value(const uint4 (&r)[6], int c) {
   const uint32_t* w = reinterpret_cast<const uint32_t*>(&r[0]);
   const uint32_t hi = w[c >> 1], lo = w[16 + (c >> 2)];
   // bytes of the value, low to high: 0, lo byte c & 3, the two of the upper half
@@ -121,15 +122,15 @@ __device__ __forceinline__ float gu_value(const uint4 (&r)[6], int c) {
   return __uint_as_float(__byte_perm(h, lo, 0x3200 | ((4 + (c & 3)) << 4)));
 }
 // The same value by its place in the buffer, for the kernels whose threads do not hold rows of it.
-__device__ __forceinline__ size_t gu_block_offset(int row, int col, int col_blocks) {
-  return ((size_t)(row >> 5) * col_blocks + (col >> 5)) * kGuBlock;
+__device__ __forceinline__ size_t kept_offset(int row, int col, int col_blocks) {
+  return ((size_t)(row >> 5) * col_blocks + (col >> 5)) * kKeptBlock;
 }
-__device__ __forceinline__ void gu_put(uint8_t* half, int r, int c, float v) {
+__device__ __forceinline__ void kept_put(uint8_t* half, int r, int c, float v) {
   const uint32_t b = __float_as_uint(v);
   *reinterpret_cast<uint16_t*>(half + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2) = (uint16_t)(b >> 16);
   half[((4 + (c >> 4)) * 32 + r) * 16 + (c & 15)] = (uint8_t)(b >> 8);
 }
-__device__ __forceinline__ float gu_get(const uint8_t* half, int r, int c) {
+__device__ __forceinline__ float kept_get(const uint8_t* half, int r, int c) {
   const uint32_t hi = *reinterpret_cast<const uint16_t*>(half + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2);
   const uint32_t lo = half[((4 + (c >> 4)) * 32 + r) * 16 + (c & 15)];
   return __uint_as_float((hi << 16) | (lo << 8));
