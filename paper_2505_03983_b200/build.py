@@ -13,6 +13,29 @@ SOURCES = ["asd_api.cu", "asd_kernels.cu", "asd_resident.cu", "asd_gemm.cu", "as
            "asd_ops_api.cu", "asd_ops_rows.cu", "asd_ops_gemm.cu", "asd_ops_stream.cu", "asd_ops_split.cu"]
 
 
+TORCH_LIB = os.path.join(HERE, "_asd_torch.so")  # the operators for torch tensors
+
+
+def _build_torch_binding(force: bool) -> None:
+    """csrc/asd_torch.cpp against this environment's torch, next to the library it calls."""
+    src = os.path.join(HERE, "csrc", "asd_torch.cpp")
+    if not force and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) >= _newest([src, os.path.join(ROOT, "include", "asd_ops.h")]):
+        return
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension as ext
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch.compiled_with_cxx11_abi()), "-DTORCH_EXTENSION_NAME=_asd_torch", "-DTORCH_API_INCLUDE_EXTENSION_H",
+           "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"]]
+    cmd += ["-I" + p for p in ext.include_paths("cuda")]
+    cmd += [src, "-o", TORCH_LIB, "-L" + HERE, "-l:libasd_b200.so", "-Wl,-rpath,$ORIGIN", "-L" + libs, "-Wl,-rpath," + libs,
+            "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch", "-ltorch_python"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed on " + src + ":\n" + res.stdout + res.stderr)
+
+
 def _newest(paths):
     return max(os.path.getmtime(p) for p in paths)
 
@@ -24,6 +47,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
                    os.path.join(HERE, "csrc", "asd_ops_internal.h"), os.path.join(HERE, "csrc", "asd_ops_tc.cuh"),
                    os.path.join(ROOT, "include", "asd.h"), os.path.join(ROOT, "include", "asd_ops.h")]
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(deps):
+        _build_torch_binding(force)
         return LIB
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
@@ -51,6 +75,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
                          capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("link failed:\n" + res.stdout + res.stderr)
+    _build_torch_binding(force)
     if verbose:
         print("".join(log))
     return LIB
