@@ -181,10 +181,8 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
   const int n_tiles = g.tiles;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
-      prefetch_tmap(&maps.p[0].a[i]);
-      prefetch_tmap(&maps.p[0].b[i]);
-    }
+    prefetch_tmap(&maps.p[0].a[0]);
+    prefetch_tmap(&maps.p[0].b[EPI == OPS_GATE ? rank : 0]);
     for (int s = 0; s < S; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
@@ -528,12 +526,10 @@ asd_status launch_pair(const asd_ops* o, const OpsGemm* list, int count, cudaStr
     p.tma_store = 1;
     for (int i = 0; i < outs; ++i)
       if (((uintptr_t)q.c[i] & 15) || (q.ldc * es) % 16) p.tma_store = 0;
-    bool ok = true;
-    for (int i = 0; i < 2; ++i) {
-      ok = ok && encode_operand(&maps.p[j].a[i], q.a[q.parts == 2 ? i : 0], q.type, I8, BM);
-      ok = ok && encode_operand(&maps.p[j].b[i], q.b[q.parts == 2 || EPI == OPS_GATE ? i : 0], q.type, I8, BN / 2);
-      if (p.tma_store) ok = ok && encode(&maps.p[j].c[i], map_type(q.type), es, q.c[i < outs ? i : 0], q.m, q.n, q.ldc, 32);
-    }
+    bool ok = true;  // only the maps that the kernel reads
+    for (int i = 0; i < q.parts; ++i) ok = ok && encode_operand(&maps.p[j].a[i], q.a[i], q.type, I8, BM);
+    for (int i = 0; i < (EPI == OPS_GATE ? 2 : q.parts); ++i) ok = ok && encode_operand(&maps.p[j].b[i], q.b[i], q.type, I8, BN / 2);
+    for (int i = 0; i < outs && p.tma_store; ++i) ok = ok && encode(&maps.p[j].c[i], map_type(q.type), es, q.c[i], q.m, q.n, q.ldc, 32);
     if (!ok) return ops_fail(ASD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   }
   const OpsGemm& q = list[0];

@@ -73,10 +73,8 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
   const uint32_t tmem_cols = g.tmem_cols;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
-      prefetch_tmap(&maps.w[i]);
-      prefetch_tmap(&maps.x[i]);
-    }
+    prefetch_tmap(&maps.w[0]);
+    prefetch_tmap(&maps.x[0]);
     for (int s = 0; s < S; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
@@ -291,11 +289,9 @@ asd_status launch_split(const asd_ops* o, const OpsGemm& q, const SplitPlan& p, 
   g.kept = q.kept, g.kept_cols = (int)((q.n + 31) / 32);
   g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias;
   g.err = o->err;
-  bool ok = true;
-  for (int i = 0; i < 2; ++i) {
-    ok = ok && encode_operand(&maps.w[i], q.b[EPI == OPS_GATE || q.parts == 2 ? i : 0], q.type, I8, F);
-    ok = ok && encode_operand(&maps.x[i], q.a[q.parts == 2 ? i : 0], q.type, I8, p.nb);
-  }
+  bool ok = true;  // only the maps that the kernel reads
+  for (int i = 0; i < (EPI == OPS_GATE ? 2 : q.parts); ++i) ok = ok && encode_operand(&maps.w[i], q.b[i], q.type, I8, F);
+  for (int i = 0; i < q.parts; ++i) ok = ok && encode_operand(&maps.x[i], q.a[i], q.type, I8, p.nb);
   if (!ok) return ops_fail(ASD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   const dim3 grid((unsigned)((q.n + F - 1) / F * p.split), (unsigned)((q.m + p.nb - 1) / p.nb));
   ops_launch(split_kernel<EPI>, grid, dim3(kSplitThreads), (size_t)split_smem(p.nb, p.stages), st, p.split, maps, g);
