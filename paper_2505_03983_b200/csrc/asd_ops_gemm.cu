@@ -556,8 +556,8 @@ int64_t pair_kblocks(const OpsGemm& q) {
   const int ke = q.epi == OPS_I8 ? 128 : 64;
   return (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
 }
-// Clocks of a launch: the tiles go to the clusters in turn, and the longest row of them counts; some 5000 to start, drain
-// the last tile and end.
+// Clocks of a launch: the tiles go to the clusters in turn, and the longest row of them counts; some 10700 to start, drain
+// the last tile and end (measured at 64 tiles of 2 to 32 k-blocks).
 double list_clocks(const asd_ops* o, const OpsGemm* list, int count, int bn) {
   const int units = o->num_sms / 2;
   double load[256] = {};
@@ -568,7 +568,7 @@ double list_clocks(const asd_ops* o, const OpsGemm* list, int count, int bn) {
     for (int u = 0; u < units; ++u) load[u] += t * (each + ((u - first % units + units) % units < tiles % units ? 1 : 0));
     first += tiles;
   }
-  return *std::max_element(load, load + units) + 5000.0;
+  return *std::max_element(load, load + units) + 10700.0;
 }
 template <int EPI>
 asd_status launch_width(const asd_ops* o, const OpsGemm* list, int count, cudaStream_t st) {

@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kSplitThreads = 64 + 256;  // a TMA warp, an MMA warp, eight epilogue warps
 constexpr int kMostStages = 8;
+constexpr int kSmSmem = 228 * 1024;  // shared memory of an SM; a block costs 1 KB beside its own
 
 struct SplitMaps {
   CUtensorMap w[2], x[2];
@@ -29,6 +30,7 @@ struct SplitArgs {
   int stages;
   int w_mn;    // the weights are read across k
   int early;   // the weights may be read before the previous kernel has ended
+  int wide;    // address and row distance of the outputs are multiples of four elements
   uint32_t idesc, tmem_cols;
   int out_type, gelu;
   void* c[2];
@@ -43,8 +45,31 @@ struct SplitArgs {
 
 __host__ __device__ constexpr int split_stage_bytes(int nb) { return (BM + nb) * 128; }
 
+__device__ __forceinline__ uint4 ld_cluster_v4(uint32_t addr) {
+  uint4 v;
+  asm("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+template <bool I8>
+__device__ __forceinline__ uint32_t add_bits(uint32_t a, uint32_t b) {
+  return I8 ? a + b : __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+}
+template <bool I8>
+__device__ __forceinline__ void add4(uint4& a, uint4 b) {
+  a = make_uint4(add_bits<I8>(a.x, b.x), add_bits<I8>(a.y, b.y), add_bits<I8>(a.z, b.z), add_bits<I8>(a.w, b.w));
+}
+// Four neighbouring 16-bit outputs; `wide`: rows and address are multiples of four elements.
+__device__ __forceinline__ void store4(void* c, int64_t at, const float (&y)[4], int cols, bool wide, bool f16) {
+  uint16_t* p = reinterpret_cast<uint16_t*>(c) + at;
+  if (wide && cols == 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack16(y[0], y[1], f16), pack16(y[2], y[3], f16));
+  } else {
+    for (int e = 0; e < cols; ++e) p[e] = round16(y[e], f16);
+  }
+}
+
 template <int EPI>
-__global__ void __launch_bounds__(kSplitThreads, 1)
+__global__ void __launch_bounds__(kSplitThreads, 3)
 split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ SplitArgs g) {
   constexpr bool I8 = EPI == OPS_I8;
   constexpr int F = EPI == OPS_GATE ? 64 : 128;  // columns of C to a CTA
@@ -58,6 +83,7 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
   uint64_t* bars = reinterpret_cast<uint64_t*>(aux);  // full[S], empty[S], acc_full
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aux + 8 * (2 * S + 1));
   volatile int* dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* row_scale = reinterpret_cast<float*>(aux + 256);  // I8: scale_a of the CTA's rows
   const uint32_t bar0 = smem_u32(bars);
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };
@@ -162,6 +188,10 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
     // ---- park this rank's partial sums as part[row][column] ----
     const int quarter = warp & 3, half = (warp - kEpiWarp0) >> 2;  // the two warps of a lane quarter take alternate groups of 16 rows
     const int feat = quarter * 32 + lane;
+    if (I8) {
+      if (g.early) grid_dependency_wait();
+      for (int r = (int)threadIdx.x - 64; r < min(g.nb, g.m - row0); r += 256) row_scale[r] = g.scale_a[row0 + r];
+    }
     mbar_wait(accf_bar, 0u, dead, g.err);
     tc_fence_after();
     uint32_t* part = reinterpret_cast<uint32_t*>(tiles_ptr);  // the stages are idle now
@@ -186,61 +216,90 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
 
   if (warp >= kEpiWarp0) {
     if (g.early) grid_dependency_wait();  // what is stored below may still be in use by an earlier kernel
+    // a thread adds up and stores four neighbouring columns, a warp whole rows of the tile
     const int tid = (int)threadIdx.x - 64;
-    const int f = tid % F, col = n0 + f;
-    constexpr int kRows = 256 / F;  // rows of C that the eight warps work on side by side
+    constexpr int kAcross = F / 4, kRows = 256 / kAcross;  // threads to a row, rows side by side
+    const int f = 4 * (tid % kAcross), col = n0 + f;
     const int m = min(g.m - row0, g.nb);
     const bool f16 = g.out_type == ASD_TYPE_F16, gelu = g.gelu != 0;
     if (col < g.n) {
-      float sb = 0.f, bb = 0.f;
+      const int cols = min(4, g.n - col);
+      float sb[4] = {}, bb[4] = {};
       if (I8) {
-        sb = g.scale_b[col];
-        bb = g.bias ? g.bias[col] : 0.f;
+        for (int e = 0; e < cols; ++e) {
+          sb[e] = g.scale_b[col + e];
+          if (g.bias) bb[e] = g.bias[col + e];
+        }
       }
-      constexpr int R = 4;  // rows whose loads are in flight together
-      for (int lr0 = rank + (tid / F) * g.split; lr0 < m; lr0 += R * kRows * g.split) {
-        uint32_t v[R], u[R];
+      constexpr int R = 2;  // rows whose loads are in flight together
+      for (int lr0 = rank + (tid / kAcross) * g.split; lr0 < m; lr0 += R * kRows * g.split) {
+        uint4 v[R], u[R];
+        float p[R][4], s[R][4];  // GATE_GRAD: the kept factors
 #pragma unroll
-        for (int i = 0; i < R; ++i) v[i] = u[i] = 0u;
+        for (int i = 0; i < R; ++i) {
+          v[i] = u[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (EPI == OPS_GATE_GRAD) {
+            const int row = row0 + min(lr0 + i * kRows * g.split, m - 1);
+            const uint8_t* b = g.kept + kept_offset(row, col, g.kept_cols);
+            kept_get4(b, row & 31, col & 31, p[i]);
+            kept_get4(b + kKeptHalf, row & 31, col & 31, s[i]);
+          }
+        }
         for (int q = 0; q < g.split; ++q) {
           const uint32_t base = map_to_cta(tiles, (uint32_t)q) + (uint32_t)(4 * f);
 #pragma unroll
           for (int i = 0; i < R; ++i) {
             const int lr = min(lr0 + i * kRows * g.split, m - 1);  // rows beyond the last are added up and not stored
-            const uint32_t p = __float_as_uint(ld_cluster_f32(base + (uint32_t)(lr * BM * 4)));
-            v[i] = I8 ? v[i] + p : __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(p));
-            if (EPI == OPS_GATE)
-              u[i] = __float_as_uint(__uint_as_float(u[i]) + ld_cluster_f32(base + (uint32_t)(lr * BM * 4 + 256)));
+            add4<I8>(v[i], ld_cluster_v4(base + (uint32_t)(lr * BM * 4)));
+            if (EPI == OPS_GATE) add4<false>(u[i], ld_cluster_v4(base + (uint32_t)(lr * BM * 4 + 256)));
           }
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
           const int row = row0 + lr0 + i * kRows * g.split;
           if (row >= row0 + m) break;
-          const float y = __uint_as_float(v[i]);
+          const float y[4] = {__uint_as_float(v[i].x), __uint_as_float(v[i].y), __uint_as_float(v[i].z), __uint_as_float(v[i].w)};
           const int64_t at = row * g.ldc + col;
           if (EPI == OPS_STORE) {
-            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(y, f16);
+            store4(g.c[0], at, y, cols, g.wide, f16);
           } else if (EPI == OPS_GATE) {
-            const float w = __uint_as_float(u[i]);
-            float a, da;
-            gate_grad(y, gelu, a, da);
+            const float w[4] = {__uint_as_float(u[i].x), __uint_as_float(u[i].y), __uint_as_float(u[i].z), __uint_as_float(u[i].w)};
+            float a[4], d[4], h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              gate_grad(y[e], gelu, a[e], d[e]);
+              h[e] = a[e] * w[e];
+              d[e] *= w[e];
+            }
             if (g.kept) {
               uint8_t* b = g.kept + kept_offset(row, col, g.kept_cols);
-              kept_put(b, row & 31, col & 31, w * da);
-              kept_put(b + kKeptHalf, row & 31, col & 31, a);
+              kept_put4(b, row & 31, col & 31, d);
+              kept_put4(b + kKeptHalf, row & 31, col & 31, a);
             }
-            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(a * w, f16);
+            store4(g.c[0], at, h, cols, g.wide, f16);
           } else if (EPI == OPS_GATE_GRAD) {
-            const uint8_t* b = g.kept + kept_offset(row, col, g.kept_cols);
-            reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(y * kept_get(b, row & 31, col & 31), f16);
-            reinterpret_cast<uint16_t*>(g.c[1])[at] = round16(y * kept_get(b + kKeptHalf, row & 31, col & 31), f16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              p[i][e] *= y[e];
+              s[i][e] *= y[e];
+            }
+            store4(g.c[0], at, p[i], cols, g.wide, f16);
+            store4(g.c[1], at, s[i], cols, g.wide, f16);
           } else {
-            const float z = fmaf((float)(int)v[i] * g.scale_a[row], sb, bb);
-            if (g.out_type == ASD_TYPE_F32)
-              reinterpret_cast<float*>(g.c[0])[at] = z;
-            else
-              reinterpret_cast<uint16_t*>(g.c[0])[at] = round16(z, f16);
+            const float sa = row_scale[row - row0];
+            const int k[4] = {(int)v[i].x, (int)v[i].y, (int)v[i].z, (int)v[i].w};
+            float z[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = fmaf((float)k[e] * sa, sb[e], bb[e]);
+            if (g.out_type == ASD_TYPE_F32) {
+              float* p = reinterpret_cast<float*>(g.c[0]) + at;
+              if (g.wide && cols == 4)
+                *reinterpret_cast<float4*>(p) = make_float4(z[0], z[1], z[2], z[3]);
+              else
+                for (int e = 0; e < cols; ++e) p[e] = z[e];
+            } else {
+              store4(g.c[0], at, z, cols, g.wide, f16);
+            }
           }
         }
       }
@@ -263,7 +322,7 @@ uint32_t split_tmem_cols(int nb) { return nb <= 32 ? 32u : (nb <= 64 ? 64u : (nb
 // bytes a column next to the 1 KB that every block costs).  CTAs that fit an SM together then never wait for one another's
 // tensor memory, which the members of a cluster, who wait for one another anyway, must not do.
 int split_smem(int nb, int stages) {
-  return std::max({stages * split_stage_bytes(nb) + 1280, nb * BM * 4 + 1280, (int)split_tmem_cols(nb) * 452});
+  return std::max(std::max(stages * split_stage_bytes(nb), nb * BM * 4) + 1024 + 256 + 1024, (int)split_tmem_cols(nb) * 452);
 }
 
 template <int EPI>
@@ -281,6 +340,8 @@ asd_status launch_split(const asd_ops* o, const OpsGemm& q, const SplitPlan& p, 
   g.tmem_cols = split_tmem_cols(p.nb);
   g.w_mn = q.b[0].mn;
   g.early = early;
+  const int es4 = 4 * ops_type_size(q.type);
+  g.wide = q.ldc % 4 == 0 && (uintptr_t)q.c[0] % es4 == 0 && (uintptr_t)q.c[1] % es4 == 0;
   const uint32_t fmt = I8 ? 1u : (q.type == ASD_TYPE_BF16 ? 1u : 0u);
   g.idesc = (I8 ? 2u << 4 : 1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)g.w_mn << 15) | ((uint32_t)(p.nb >> 3) << 17) |
             ((uint32_t)(BM >> 4) << 24);
@@ -305,32 +366,37 @@ cudaError_t prepare_split() {
 
 }  // namespace
 
-// The cheapest way to split.  Clocks of a CTA: its k-blocks at the larger of the MMAs' time (nb / 128 of 256 clocks) and
-// its share of the SM's way into shared memory (some 50 bytes a clock), then some 3000 to join the partial sums and start
-// and end, and 8 for each row that a CTA adds up.
+// The cheapest way to split, by an estimate in clocks that was fitted to 9 shapes of 16 to 2000 rows (int8, k 208 to 4096, out
+// 1000 to 8192), each with every split; what it picks is within 10 % of the best of them.  A CTA's k-blocks cost the larger
+// of its MMAs' time (2 clocks a row) and its operands' way into shared memory (64 bytes a clock and SM); parking, adding up
+// and storing cost 37 clocks a row; starting and ending 7000, joining a cluster of two or four 2500 more, and of eight,
+// which the GPU finds room for slowly, 9000.
 SplitPlan plan_split(const asd_ops* o, const OpsGemm& q) {
   const int ke = q.epi == OPS_I8 ? 128 : 64, F = q.epi == OPS_GATE ? 64 : 128;
   const int64_t kb = (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
   const int64_t tiles_n = (q.n + F - 1) / F;
   SplitPlan best{16, 1, 2, 1e300};
-  for (int blocks = (int)((q.m + 255) / 256); blocks <= (int)((q.m + 255) / 256) + 8; ++blocks) {
+  const int64_t least = (q.m + 255) / 256;
+  for (int64_t blocks = least; blocks <= 4 * least + 16; ++blocks) {
     const int nb = (int)std::max<int64_t>(16, ((q.m + blocks - 1) / blocks + 15) / 16 * 16);
     if (nb > 256) continue;
     const int64_t tiles_m = (q.m + nb - 1) / nb;
     for (int split = 1; split <= 8; split *= 2) {
       if (split > 1 && kb / split < 2) break;
-      const int64_t ctas = tiles_n * tiles_m * split;
-      // two CTAs to an SM where their shared memory allows it and there are enough of them
-      const int two = nb <= 128 && ctas > o->num_sms ? 2 : 1;
-      const int64_t waves = (ctas + two * o->num_sms - 1) / (two * o->num_sms);
-      const double fill = two * (BM + nb) * 128 / 50.0, math = two * std::max(128.0, 2.0 * nb);
-      const double t = waves * ((double)((kb + split - 1) / split) * std::max(fill, math) + 3000.0 + 8.0 * nb / split * split);
+      const int64_t ctas = tiles_n * tiles_m * split, share = (kb + split - 1) / split;
+      // CTAs that run side by side on an SM
+      int side = (int)std::min<int64_t>(3, (ctas + o->num_sms - 1) / o->num_sms);
+      while (side > 1 && side * (split_smem(nb, 2) + 1024) > kSmSmem) --side;
+      const int64_t waves = (ctas + side * o->num_sms - 1) / (side * o->num_sms);
+      const double fill = side * (BM + nb) * 128 / 64.0, math = side * std::max(128.0, 2.0 * nb);
+      const double t = 7000.0 + (split == 8 ? 9000.0 : split > 1 ? 2500.0 : 0.0) + waves * (share * std::max(fill, math) + 37.0 * nb / split);
       if (t < best.clocks) {
-        const int budget = two == 2 ? 110 * 1024 : 220 * 1024;
-        const int stages = std::max(2, std::min({kMostStages, budget / split_stage_bytes(nb), (int)std::max<int64_t>(2, (kb + split - 1) / split)}));
+        int stages = (int)std::min<int64_t>(kMostStages, std::max<int64_t>(2, share));
+        while (stages > 2 && side * (split_smem(nb, stages) + 1024) > kSmSmem) --stages;
         best = SplitPlan{nb, split, stages, t};
       }
     }
+    if (nb == 16) break;
   }
   return best;
 }

@@ -130,10 +130,22 @@ __device__ __forceinline__ void kept_put(uint8_t* half, int r, int c, float v) {
   *reinterpret_cast<uint16_t*>(half + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2) = (uint16_t)(b >> 16);
   half[((4 + (c >> 4)) * 32 + r) * 16 + (c & 15)] = (uint8_t)(b >> 8);
 }
-__device__ __forceinline__ float kept_get(const uint8_t* half, int r, int c) {
-  const uint32_t hi = *reinterpret_cast<const uint16_t*>(half + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2);
-  const uint32_t lo = half[((4 + (c >> 4)) * 32 + r) * 16 + (c & 15)];
-  return __uint_as_float((hi << 16) | (lo << 8));
+// Four neighbouring columns from a multiple of four.
+__device__ __forceinline__ void kept_put4(uint8_t* half, int r, int c, const float (&v)[4]) {
+  uint32_t b[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) b[e] = __float_as_uint(v[e]);
+  *reinterpret_cast<uint2*>(half + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2) = make_uint2(__byte_perm(b[0], b[1], 0x7632), __byte_perm(b[2], b[3], 0x7632));
+  *reinterpret_cast<uint32_t*>(half + ((4 + (c >> 4)) * 32 + r) * 16 + (c & 15)) =
+      __byte_perm(__byte_perm(b[0], b[1], 0x0051), __byte_perm(b[2], b[3], 0x0051), 0x5410);
+}
+__device__ __forceinline__ void kept_get4(const uint8_t* half, int r, int c, float (&v)[4]) {
+  const uint2 hi = *reinterpret_cast<const uint2*>(half + ((c >> 3) * 32 + r) * 16 + (c & 7) * 2);
+  const uint32_t lo = *reinterpret_cast<const uint32_t*>(half + ((4 + (c >> 4)) * 32 + r) * 16 + (c & 15));
+  v[0] = __uint_as_float((hi.x << 16) | ((lo & 0xffu) << 8));
+  v[1] = __uint_as_float((hi.x & 0xffff0000u) | (lo & 0xff00u));
+  v[2] = __uint_as_float((hi.y << 16) | ((lo >> 8) & 0xff00u));
+  v[3] = __uint_as_float((hi.y & 0xffff0000u) | ((lo >> 16) & 0xff00u));
 }
 
 }  // namespace
