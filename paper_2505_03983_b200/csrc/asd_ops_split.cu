@@ -369,8 +369,8 @@ cudaError_t prepare_split() {
 // The cheapest way to split, by an estimate in clocks that was fitted to 9 shapes of 16 to 2000 rows (int8, k 208 to 4096, out
 // 1000 to 8192), each with every split; what it picks is within 10 % of the best of them.  A CTA's k-blocks cost the larger
 // of its MMAs' time (2 clocks a row) and its operands' way into shared memory (64 bytes a clock and SM); parking, adding up
-// and storing cost 37 clocks a row; starting and ending 7000, joining a cluster of two or four 2500 more, and of eight,
-// which the GPU finds room for slowly, 9000.
+// and storing cost 37 clocks a row; a launch 3000 and each wave of CTAs 4000; joining a cluster of two or four 2500 more,
+// and of eight, which the GPU finds room for slowly, 9000.
 SplitPlan plan_split(const asd_ops* o, const OpsGemm& q) {
   const int ke = q.epi == OPS_I8 ? 128 : 64, F = q.epi == OPS_GATE ? 64 : 128;
   const int64_t kb = (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
@@ -389,7 +389,8 @@ SplitPlan plan_split(const asd_ops* o, const OpsGemm& q) {
       while (side > 1 && side * (split_smem(nb, 2) + 1024) > kSmSmem) --side;
       const int64_t waves = (ctas + side * o->num_sms - 1) / (side * o->num_sms);
       const double fill = side * (BM + nb) * 128 / 64.0, math = side * std::max(128.0, 2.0 * nb);
-      const double t = 7000.0 + (split == 8 ? 9000.0 : split > 1 ? 2500.0 : 0.0) + waves * (share * std::max(fill, math) + 37.0 * nb / split);
+      const double join = split == 8 ? 9000.0 : split > 1 ? 2500.0 : 0.0;
+      const double t = 3000.0 + waves * (4000.0 + join + share * std::max(fill, math) + 37.0 * nb / split);
       if (t < best.clocks) {
         int stages = (int)std::min<int64_t>(kMostStages, std::max<int64_t>(2, share));
         while (stages > 2 && side * (split_smem(nb, stages) + 1024) > kSmSmem) --stages;
