@@ -587,9 +587,9 @@ int64_t gated_kept_bytes(int64_t rows, int64_t hidden) { return (rows + 31) / 32
 
 namespace {
 // Whether a product is better split than tiled; `plan` is how.
-bool better_split(const asd_ops* o, const OpsGemm& q, SplitPlan* plan) {
+bool better_split(const asd_ops* o, const OpsGemm& q, bool early, SplitPlan* plan) {
   if (q.a[0].mn) return false;
-  *plan = plan_split(o, q);
+  *plan = plan_split(o, q, early);
   return plan->clocks < std::min(list_clocks(o, &q, 1, 256), list_clocks(o, &q, 1, 128));
 }
 }  // namespace
@@ -597,7 +597,7 @@ bool better_split(const asd_ops* o, const OpsGemm& q, SplitPlan* plan) {
 asd_status ops_gemm(const asd_ops* o, const OpsGemm& q, bool early, cudaStream_t st) {
   if (use_stream(q)) return ops_gemm_stream(o, q, early, st);
   SplitPlan p;
-  if (better_split(o, q, &p)) return ops_gemm_split(o, q, p, early, st);
+  if (better_split(o, q, early, &p)) return ops_gemm_split(o, q, p, early, st);
   switch (q.epi) {
     case OPS_STORE: return launch_width<OPS_STORE>(o, &q, 1, st);
     case OPS_GATE: return launch_width<OPS_GATE>(o, &q, 1, st);
@@ -611,7 +611,7 @@ asd_status ops_gemm(const asd_ops* o, const OpsGemm& q, bool early, cudaStream_t
 // depend on the others, so that a gradient has the same bits whichever are asked for.
 asd_status ops_gemm_list(const asd_ops* o, const OpsGemm* list, int count, cudaStream_t st) {
   SplitPlan p;
-  if (count && better_split(o, list[0], &p)) {
+  if (count && better_split(o, list[0], false, &p)) {
     const asd_status s = ops_gemm_split(o, list[0], p, false, st);
     if (s != ASD_OK) return s;
     ++list, --count;

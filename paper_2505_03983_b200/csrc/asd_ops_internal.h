@@ -112,7 +112,7 @@ struct SplitPlan {
   int nb, split, stages;  // rows of a CTA, CTAs that share a sum, stages of its operands
   double clocks;          // estimate
 };
-SplitPlan plan_split(const asd_ops* o, const OpsGemm& g);
+SplitPlan plan_split(const asd_ops* o, const OpsGemm& g, bool early);
 asd_status ops_split_prepare();
 asd_status ops_gemm_split(const asd_ops* o, const OpsGemm& g, const SplitPlan& p, bool early, cudaStream_t st);
 

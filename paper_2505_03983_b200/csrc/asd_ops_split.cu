@@ -117,7 +117,10 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  if (!g.early) grid_dependency_wait();
+  if (!g.early) {
+    grid_dependency_wait();
+    grid_launch_dependents();  // the next kernel may fetch its weights beside this one
+  }
 
   if (warp == 0) {
     // ---------------- TMA producer ----------------
@@ -212,7 +215,7 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
   __syncthreads();
   __syncwarp();
   cluster_sync_all();  // every rank's partial sums are in place
-  grid_launch_dependents();
+  if (g.early) grid_launch_dependents();  // after the wait above: what the next one may read early is then complete
 
   if (warp >= kEpiWarp0) {
     if (g.early) grid_dependency_wait();  // what is stored below may still be in use by an earlier kernel
@@ -366,15 +369,17 @@ cudaError_t prepare_split() {
 
 }  // namespace
 
-// The cheapest way to split, by an estimate in clocks that was fitted to 9 shapes of 16 to 2000 rows (int8, k 208 to 4096, out
-// 1000 to 8192), each with every split; what it picks is within 10 % of the best of them.  A CTA's k-blocks cost the larger
-// of its MMAs' time (2 clocks a row) and its operands' way into shared memory (64 bytes a clock and SM); parking, adding up
-// and storing cost 37 clocks a row; a launch 3000 and each wave of CTAs 4000; joining a cluster of two or four 2500 more,
-// and of eight, which the GPU finds room for slowly, 9000.
-SplitPlan plan_split(const asd_ops* o, const OpsGemm& q) {
+// The cheapest way to split, by an estimate in clocks that was fitted to 13 shapes of 16 to 2000 rows (int8 and 16 bits, k
+// 208 to 8192, out 1000 to 16384), each with every split; what it picks is within 10 % of the best of them.  A CTA's
+// k-blocks cost the largest of its MMAs' time (2 clocks a row), its operands' way into shared memory (64 bytes a clock and
+// SM) and the weights' way from memory (23 bytes a clock and SM that has a CTA).  Parking, adding up and storing cost 37
+// clocks a row; a launch 3000 and each wave of CTAs 4000; joining a cluster 2500 more, and one of eight, which the GPU finds
+// room for slowly, 9000 unless that is hidden under the kernel before (`early`).
+SplitPlan plan_split(const asd_ops* o, const OpsGemm& q, bool early) {
   const int ke = q.epi == OPS_I8 ? 128 : 64, F = q.epi == OPS_GATE ? 64 : 128;
   const int64_t kb = (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
   const int64_t tiles_n = (q.n + F - 1) / F;
+  const double weights = (double)tiles_n * kb * BM * 128;
   SplitPlan best{16, 1, 2, 1e300};
   const int64_t least = (q.m + 255) / 256;
   for (int64_t blocks = least; blocks <= 4 * least + 16; ++blocks) {
@@ -389,10 +394,12 @@ SplitPlan plan_split(const asd_ops* o, const OpsGemm& q) {
       while (side > 1 && side * (split_smem(nb, 2) + 1024) > kSmSmem) --side;
       const int64_t waves = (ctas + side * o->num_sms - 1) / (side * o->num_sms);
       const double fill = side * (BM + nb) * 128 / 64.0, math = side * std::max(128.0, 2.0 * nb);
-      const double join = split == 8 ? 9000.0 : split > 1 ? 2500.0 : 0.0;
-      const double t = 3000.0 + waves * (4000.0 + join + share * std::max(fill, math) + 37.0 * nb / split);
+      const double stream = weights / (23.0 * std::min<int64_t>(ctas, o->num_sms)) / waves;
+      const double join = split == 8 && !early ? 9000.0 : split > 1 ? 2500.0 : 0.0;
+      const double t = 3000.0 + waves * (4000.0 + join + std::max(stream, share * std::max(fill, math)) + 37.0 * nb / split);
       if (t < best.clocks) {
-        int stages = (int)std::min<int64_t>(kMostStages, std::max<int64_t>(2, share));
+        // few rows: no more than half of the SM's shared memory, which leaves room for the next kernel's first weights
+        int stages = (int)std::min<int64_t>(nb <= 64 ? 112 * 1024 / split_stage_bytes(nb) : kMostStages, std::max<int64_t>(2, share));
         while (stages > 2 && side * (split_smem(nb, stages) + 1024) > kSmSmem) --stages;
         best = SplitPlan{nb, split, stages, t};
       }

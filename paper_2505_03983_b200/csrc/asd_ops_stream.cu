@@ -17,7 +17,9 @@ namespace {
 
 constexpr int kStreamWarps = 16;
 
-constexpr int kStreamSmem = 232448 - 2 * kStreamWarps * 8 * 17 * 4;  // of a block, without the partial sums
+constexpr int kStreamSmem = 232448;
+// Shared memory of x and the partial sums.
+int64_t rows_bytes(int64_t rows, int64_t pitch) { return rows * (pitch + 2 * kStreamWarps * 17 * 4); }
 constexpr int ring_bytes(int ring) { return kStreamWarps * ring * 1024; }
 
 struct StreamArgs {
@@ -76,8 +78,7 @@ __device__ __forceinline__ void mma_16x8(uint32_t (&c)[4], uint32_t a0, uint32_t
 template <int KIND, int EPI, int RING>
 __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const StreamArgs a) {
   constexpr int FR = EPI == OPS_GATE ? 8 : 16;  // columns of the output to a group of rows of w
-  extern __shared__ __align__(128) uint8_t smem[];  // the warps' rings, then x
-  __shared__ uint32_t part[2][kStreamWarps][8][17];  // a warp's sums: [row of x][row of w]
+  extern __shared__ __align__(128) uint8_t smem[];  // the warps' rings, x, the warps' sums
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int units = (a.n + FR - 1) / FR;
   const int mine = ((int)blockIdx.x < units) ? (units - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;
@@ -88,6 +89,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
   uint8_t* ring = smem + warp * (RING * 1024) + lane * 16;
   const uint32_t ring_addr = smem_u32(ring);
   uint8_t* xs = smem + kStreamWarps * RING * 1024;
+  // a warp's sums, [2][warp][row of x][16 rows of w and one word that keeps rows on different banks]
+  uint32_t* part = reinterpret_cast<uint32_t*>(xs + a.rows * a.pitch);
 
   // The copies run ahead of the sums through the same sequence: steps s0 .. s1 of the block's first rows, then of its next.
   int unit = s0 < s1 ? 0 : mine, step = s0, slot = 0;
@@ -143,18 +146,26 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
       mma_16x8<KIND>(acc, c0.z, c1.z, c0.w, c1.w, x.z, x.w);
       if (++at == RING) at = 0;
     }
-    uint32_t(*p)[8][17] = part[i & 1];  // free: every thread has passed the barrier of unit i - 1 after reading unit i - 2's
-    p[warp][2 * t][g] = acc[0];
-    p[warp][2 * t + 1][g] = acc[1];
-    p[warp][2 * t][g + 8] = acc[2];
-    p[warp][2 * t + 1][g + 8] = acc[3];
+    // free: every thread has passed the barrier of unit i - 1 after reading unit i - 2's
+    const int of_row = 17, of_warp = a.rows * 17;
+    uint32_t* p = part + (i & 1) * kStreamWarps * of_warp;
+    uint32_t* own = p + warp * of_warp + g;
+    if (2 * t < a.rows) {
+      own[2 * t * of_row] = acc[0];
+      own[2 * t * of_row + 8] = acc[2];
+    }
+    if (2 * t + 1 < a.rows) {
+      own[(2 * t + 1) * of_row] = acc[1];
+      own[(2 * t + 1) * of_row + 8] = acc[3];
+    }
     __syncthreads();
     const int f = threadIdx.x % FR, row = threadIdx.x / FR, col = ((int)blockIdx.x + i * (int)gridDim.x) * FR + f;
     if (row >= a.rows || col >= a.n) continue;
+    const uint32_t* sums = p + row * of_row + f;
     if constexpr (KIND == KIND_I8) {
       int v = 0;
 #pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) v += (int)p[w][row][f];
+      for (int w = 0; w < kStreamWarps; ++w) v += (int)sums[w * of_warp];
       const float y = fmaf((float)v * a.scale_a[row], a.scale_b[col], a.bias ? a.bias[col] : 0.f);
       if (a.out_type == ASD_TYPE_F32)
         reinterpret_cast<float*>(a.c)[row * a.ldc + col] = y;
@@ -164,8 +175,8 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
       float v = 0.f, u = 0.f;
 #pragma unroll
       for (int w = 0; w < kStreamWarps; ++w) {
-        v += __uint_as_float(p[w][row][f]);
-        if (EPI == OPS_GATE) u += __uint_as_float(p[w][row][f + 8]);
+        v += __uint_as_float(sums[w * of_warp]);
+        if (EPI == OPS_GATE) u += __uint_as_float(sums[w * of_warp + 8]);
       }
       if (EPI == OPS_GATE) {
         float act, slope;
@@ -186,10 +197,14 @@ template <int KIND, int EPI>
 void launch_stream(const asd_ops* o, const StreamArgs& a, cudaStream_t st) {
   const int fr = EPI == OPS_GATE ? 8 : 16;
   const dim3 grid(std::min((a.n + fr - 1) / fr, o->num_sms)), block(32 * kStreamWarps);
-  const int x = a.rows * a.pitch;  // what x leaves is the ring's
-  if (x <= kStreamSmem - ring_bytes(12))
+  const int x = (int)rows_bytes(a.rows, a.pitch);
+  // The ring: no longer than a warp has steps, so that the next kernel's blocks find room beside these; of a kernel that
+  // may start early the shortest, for it has to fit beside the one before.
+  const int units = (a.n + fr - 1) / fr, steps = (a.k_bytes + 63) / 64;
+  const int most = (units + (int)grid.x - 1) / (int)grid.x * ((steps + kStreamWarps - 1) / kStreamWarps);
+  if (x <= kStreamSmem - ring_bytes(12) && most > 8 && !a.early)
     ops_launch(stream_kernel<KIND, EPI, 12>, grid, block, (size_t)(ring_bytes(12) + x), st, 1, a);
-  else if (x <= kStreamSmem - ring_bytes(8))
+  else if (x <= kStreamSmem - ring_bytes(8) && most > 4 && !a.early)
     ops_launch(stream_kernel<KIND, EPI, 8>, grid, block, (size_t)(ring_bytes(8) + x), st, 1, a);
   else
     ops_launch(stream_kernel<KIND, EPI, 4>, grid, block, (size_t)(ring_bytes(4) + x), st, 1, a);
@@ -211,7 +226,7 @@ int x_pitch(int64_t k_bytes) { return (int)((k_bytes + 127) / 128 * 128 + 64); }
 bool use_stream(const OpsGemm& q) {
   const int es = q.epi == OPS_I8 ? 1 : 2;
   return (q.epi == OPS_GATE || q.epi == OPS_I8 || (q.epi == OPS_STORE && q.parts == 1)) && q.m <= kStreamMaxRows &&
-         !q.a[0].mn && !q.b[0].mn && q.m * x_pitch(q.k[0] * es) <= kStreamSmem - ring_bytes(4);
+         !q.a[0].mn && !q.b[0].mn && rows_bytes(q.m, x_pitch(q.k[0] * es)) <= kStreamSmem - ring_bytes(4);
 }
 
 asd_status ops_gemm_stream(const asd_ops* o, const OpsGemm& q, bool early, cudaStream_t st) {

@@ -193,14 +193,19 @@ class AsdOps:
 
 
 _DEFAULT = {}
+_current_device = None
 
 
 def default_ops() -> AsdOps:
     """The process's handle of the current device, made at its first use."""
-    import torch
-    if not torch.cuda.is_available():
-        raise AsdError(4, "no CUDA device: the ASD library has no CPU path")
-    device = torch.cuda.current_device()
-    if device not in _DEFAULT:
-        _DEFAULT[device] = AsdOps()
-    return _DEFAULT[device]
+    global _current_device
+    if _current_device is None:
+        import torch
+        if not torch.cuda.is_available():
+            raise AsdError(4, "no CUDA device: the ASD library has no CPU path")
+        _current_device = torch.cuda.current_device
+    device = _current_device()
+    ops = _DEFAULT.get(device)
+    if ops is None:
+        ops = _DEFAULT[device] = AsdOps()
+    return ops
