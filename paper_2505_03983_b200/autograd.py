@@ -1,0 +1,52 @@
+"""The operators that have gradients, as torch.autograd functions of the current device's handle.
+
+    y, s = add_rmsnorm(x, weight, residual)      y = norm(x + residual) * weight, s = x + residual
+    y = gated_mlp(x, w_in, w_out, act)           y = (act(x Wg^T) * (x Wu^T)) w_out^T
+"""
+from __future__ import annotations
+
+import torch
+
+from .operators import default_ops
+
+
+class _AddRmsnorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        y, s = default_ops().add_rmsnorm(x, weight, residual=residual, eps=eps)
+        ctx.save_for_backward(s, weight)
+        ctx.eps, ctx.has_residual = eps, residual is not None
+        return y, s if residual is not None else s.view_as(s)  # without a residual s is x: an output of its own
+
+    @staticmethod
+    def backward(ctx, dy, ds):
+        s, weight = ctx.saved_tensors
+        need_dw = weight is not None and ctx.needs_input_grad[1]
+        dx, dw = default_ops().add_rmsnorm_backward(dy, s, weight, ds=ds, eps=ctx.eps, need_dweight=need_dw)
+        return dx, dw, dx if ctx.has_residual else None, None
+
+
+class _GatedMlp(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_in, w_out, act):
+        ctx.act = act
+        if not any(ctx.needs_input_grad):
+            return default_ops().gated_mlp(x, w_in, w_out, act=act)
+        y, saved = default_ops().gated_mlp_forward(x, w_in, w_out, act=act)
+        ctx.save_for_backward(x, w_in, w_out, saved)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w_in, w_out, saved = ctx.saved_tensors
+        return (*default_ops().gated_mlp_backward(dy, x, w_in, w_out, saved, act=ctx.act, need=ctx.needs_input_grad[:3]), None)
+
+
+def add_rmsnorm(x, weight, residual=None, eps=1e-6):
+    """AsdOps.add_rmsnorm with gradients in x, weight and residual."""
+    return _AddRmsnorm.apply(x, weight, residual, eps)
+
+
+def gated_mlp(x, w_in, w_out, act="silu"):
+    """AsdOps.gated_mlp with gradients in x, w_in and w_out."""
+    return _GatedMlp.apply(x, w_in, w_out, act)
