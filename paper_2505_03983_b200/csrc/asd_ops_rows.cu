@@ -6,7 +6,7 @@
 // belongs to 32, 128, 256 or 512 threads (rows of up to 1024, 4096, 8192, 16384), 32 elements to a thread, so that a thread has its
 // 16-byte loads in flight together; longer rows are read a second time.  A row whose address, distance or length is not a
 // multiple of 8 elements is read element by element, neighbouring threads on neighbouring elements.
-#include <float.h>
+#include <type_traits>
 
 #include "asd_ops_internal.h"
 
@@ -161,6 +161,39 @@ __device__ __forceinline__ float act_value(float g, int act) {
   return 0.5f * g * (1.f + erff(g * 0.7071067811865476f));
 }
 
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 c;
+  asm("{\n\t.reg .b64 pa, pb, pc;\n\tmov.b64 pa, {%2, %3};\n\tmov.b64 pb, {%4, %5};\n\tmul.rn.f32x2 pc, pa, pb;\n\tmov.b64 {%0, %1}, pc;\n\t}"
+      : "=f"(c.x), "=f"(c.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 pa, pb, pc, pd;\n\tmov.b64 pa, {%2, %3};\n\tmov.b64 pb, {%4, %5};\n\tmov.b64 pc, {%6, %7};\n\t"
+      "fma.rn.f32x2 pd, pa, pb, pc;\n\tmov.b64 {%0, %1}, pd;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+// Pair i of elements that are held as they are stored.
+template <typename T>
+__device__ __forceinline__ float2 unpack(const uint32_t* e, int i) {
+  if constexpr (sizeof(T) == 4)
+    return make_float2(__uint_as_float(e[2 * i]), __uint_as_float(e[2 * i + 1]));
+  else if constexpr (std::is_same<T, __nv_bfloat16>::value)
+    return make_float2(__uint_as_float(e[i] << 16), __uint_as_float(e[i] & 0xffff0000u));
+  else
+    return __half22float2(*reinterpret_cast<const __half2*>(e + i));
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 c;
+  asm("{\n\t.reg .b64 pa, pb, pc;\n\tmov.b64 pa, {%2, %3};\n\tmov.b64 pb, {%4, %5};\n\tadd.rn.f32x2 pc, pa, pb;\n\tmov.b64 {%0, %1}, pc;\n\t}"
+      : "=f"(c.x), "=f"(c.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+
 struct NormArgs {
   int rows, width, w_f32;
   float eps;
@@ -289,6 +322,24 @@ __global__ void __launch_bounds__(block_of<TPR>) rmsnorm_kernel(const NormArgs a
   }
 }
 
+// act(g) u for two elements: the same operations as act_value's.
+__device__ __forceinline__ float2 gated2(float2 g, float2 u, int act) {
+  float2 a;
+  if (act == ASD_ACT_SILU) {
+    const float2 x = mul2(g, make_float2(-1.4426950408889634f, -1.4426950408889634f));
+    float2 e, p;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(x.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(x.y));
+    e = add2(e, make_float2(1.f, 1.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p.y) : "f"(e.y));
+    a = mul2(g, p);
+  } else {
+    a = make_float2(act_value(g.x, act), act_value(g.y, act));
+  }
+  return mul2(a, u);
+}
+
 struct QuantArgs {
   int rows, width, act, stride;  // stride: rows that are worked on side by side
   const void* x;
@@ -349,12 +400,25 @@ __global__ void __launch_bounds__(block_of<TPR>) quantize_kernel(const QuantArgs
     for (int v = 0; v < NV; ++v) {
       const int col = (v * TPR + t) * VEC;
       if (col < a.width) {
-        load_vec<VEC, T>(AHEAD ? reinterpret_cast<const T*>(slot(turn, 0, v)) : x + col, f[v]);
-        if (gate) {
-          float u[VEC];
-          load_vec<VEC, T>(AHEAD ? reinterpret_cast<const T*>(slot(turn, 1, v)) : x + a.width + col, u);
+        if constexpr (AHEAD) {
+          uint32_t g[4], u[4];
+          *reinterpret_cast<uint4*>(g) = *slot(turn, 0, v);
+          if (gate) *reinterpret_cast<uint4*>(u) = *slot(turn, 1, v);
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) f[v][i] = act_value(f[v][i], a.act) * u[i];
+          for (int i = 0; i < 4; ++i) {
+            float2 h = unpack<T>(g, i);
+            if (gate) h = gated2(h, unpack<T>(u, i), a.act);
+            f[v][2 * i] = h.x;
+            f[v][2 * i + 1] = h.y;
+          }
+        } else {
+          load_vec<VEC, T>(x + col, f[v]);
+          if (gate) {
+            float u[VEC];
+            load_vec<VEC, T>(x + a.width + col, u);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f[v][i] = act_value(f[v][i], a.act) * u[i];
+          }
         }
 #pragma unroll
         for (int i = 0; i < VEC; ++i) most = max(most, mag(f[v][i]));
@@ -416,125 +480,156 @@ struct NormGradArgs {
   int64_t ld_dy, ld_s, ld_ds, ld_dx;
 };
 
-// VEC elements as they are stored.
-template <typename T, int VEC>
-struct RawVec {
-  uint4 v[sizeof(T) * VEC / 16];
-};
-template <typename T>
-struct RawVec<T, 1> {
-  T v[1];
-};
-template <int VEC, typename T>
-__device__ __forceinline__ RawVec<T, VEC> load_raw(const T* p) {
-  RawVec<T, VEC> r;
-  if constexpr (VEC == 1) {
-    r.v[0] = *p;
-  } else {
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(r.v) / 16); ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
-  }
-  return r;
-}
-template <typename T, int VEC>
-__device__ __forceinline__ float raw_at(const RawVec<T, VEC>& r, int i) {
-  return to_f<T>(reinterpret_cast<const T*>(&r.v[0])[i]);
-}
-
 // Gradients.  One block walks over rows blockIdx.x, + blocks, ...; a thread keeps the same columns in every row, so the
 // weights and the sums of dw over the block's rows stay in its registers; the sums are written once, to be added up by
-// reduce_dw_kernel.  Both sums of a row, of s^2 and of dy w s, are taken together: mean(dy w z) = rho mean(dy w s).  The next
-// row's loads (kept as they are stored) are issued before a row's sums meet, so that memory is busy over the barrier.
+// reduce_dw_kernel.  Both sums of a row, of s^2 and of dy w s, are taken together: mean(dy w z) = rho mean(dy w s).  Rows
+// that can be read in 16-byte pieces come through shared memory two rows ahead (32 bits: one) (cp.async; a thread reads back only
+// what it has copied itself), so that memory is busy over the barriers; the others are read where they are needed.
+template <typename T>
+constexpr int grad_ahead = sizeof(T) == 2 ? 2 : 1;
+template <typename T, int VEC, int TPR, int PER>
+constexpr int grad_smem = VEC == 8 ? (grad_ahead<T> + 1) * 3 * PER * (int)sizeof(T) * TPR : 0;
+
 template <typename T, int VEC, int TPR, int PER>
 __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a) {
-  constexpr int NV = PER / VEC;
+  // elements come in groups of E: VEC neighbouring ones, or (VEC = 1) two that are TPR apart
+  constexpr int E = VEC == 1 ? 2 : VEC, NV = PER / E, NP = E / 2;  // NP: pairs; every product and sum is a two-way fp32 instruction
+  constexpr bool AHEAD = VEC == 8;
+  constexpr int kGradAhead = grad_ahead<T>;
+  constexpr int PIECES = VEC * (int)sizeof(T) / 16;  // of 16 bytes to VEC elements
+  extern __shared__ __align__(16) uint4 ahead[];      // [row][s, dy, ds][NV][pieces][threads]
   __shared__ float buf[2][2][TPR / 32];
   dep_wait();
   dep_launch();
   const int t = threadIdx.x;
-  float acc[NV][VEC], w[NV][VEC];
+  auto column = [&](int v, int i) { return VEC == 1 ? (2 * v + i) * TPR + t : (v * TPR + t) * VEC + i; };
+  float2 acc[NV][NP], w[NV][NP];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int col = (v * TPR + t) * VEC;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) acc[v][i] = w[v][i] = 0.f;
-    if (col < a.width) load_weight<VEC, T>(a.w, a.w_f32, col, w[v]);
-  }
-  struct Row {
-    RawVec<T, VEC> s[NV], dy[NV], ds[NV];
-  };
-  auto fetch = [&](int64_t row, Row& r) {
-    const T* s = reinterpret_cast<const T*>(a.s) + row * a.ld_s;
-    const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.ld_dy;
-    const T* ds = reinterpret_cast<const T*>(a.ds) + row * a.ld_ds;
+    for (int i = 0; i < NP; ++i) {
+      float one[2] = {0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * TPR + t) * VEC;
-      if (col < a.width) {
-        r.s[v] = load_raw<VEC, T>(s + col);
-        r.dy[v] = load_raw<VEC, T>(dy + col);
-        if (a.ds) r.ds[v] = load_raw<VEC, T>(ds + col);
+      for (int e = 0; e < 2; ++e) {
+        float f[1];
+        if (column(v, 2 * i + e) < a.width) {
+          load_weight<1, T>(a.w, a.w_f32, column(v, 2 * i + e), f);
+          one[e] = f[0];
+        }
       }
+      acc[v][i] = make_float2(0.f, 0.f);
+      w[v][i] = make_float2(one[0], one[1]);
     }
-  };
-  Row cur, next;
-  int turn = 0;
-  if (blockIdx.x < a.rows) fetch(blockIdx.x, cur);
-  for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks, turn ^= 1) {
-    if (row + a.blocks < a.rows) fetch(row + a.blocks, next);
-    float sq = 0.f, dot = 0.f;
+  }
+  const T* base[3] = {reinterpret_cast<const T*>(a.s), reinterpret_cast<const T*>(a.dy), reinterpret_cast<const T*>(a.ds)};
+  const int64_t ld[3] = {a.ld_s, a.ld_dy, a.ld_ds};
+  auto slot = [&](int turn, int part, int v, int piece) { return ahead + (((turn * 3 + part) * NV + v) * PIECES + piece) * TPR + t; };
+  auto fetch = [&](int64_t row, int turn) {
+    if (row < a.rows) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if ((v * TPR + t) * VEC < a.width) {
+      for (int v = 0; v < NV; ++v) {
+        const int col = column(v, 0);
+        if (col < a.width) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float f = raw_at(cur.s[v], i);
-          sq = fmaf(f, f, sq);
-          dot = fmaf(raw_at(cur.dy[v], i) * w[v][i], f, dot);
+          for (int part = 0; part < 3; ++part)
+            if (part < 2 || a.ds) {
+#pragma unroll
+              for (int k = 0; k < PIECES; ++k)
+                copy_16((uint32_t)__cvta_generic_to_shared(slot(turn, part, v, k)), base[part] + row * ld[part] + col + k * (16 / (int)sizeof(T)));
+            }
         }
       }
     }
-    sq = warp_sum(sq);
-    dot = warp_sum(dot);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // VEC elements of s (0), dy (1) or ds (2) of the row that is worked on
+  auto read = [&](int64_t row, int turn, int part, int v, int col, float2(&f)[NP]) {
+    if constexpr (AHEAD) {
+      uint32_t e[4 * PIECES];
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) reinterpret_cast<uint4*>(e)[k] = *slot(turn, part, v, k);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) f[i] = unpack<T>(e, i);
+    } else {
+      const T* p = base[part] + row * ld[part] + col;
+      f[0] = make_float2(to_f<T>(p[0]), col + TPR < a.width ? to_f<T>(p[TPR]) : 0.f);
+    }
+  };
+  if (AHEAD) {
+#pragma unroll
+    for (int k = 0; k < kGradAhead; ++k) fetch(blockIdx.x + (int64_t)k * a.blocks, k);
+  }
+  int turn = 0, side = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks, side ^= 1) {
+    if (AHEAD) {
+      fetch(row + (int64_t)kGradAhead * a.blocks, turn == 0 ? kGradAhead : turn - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kGradAhead) : "memory");
+    }
+    float2 f[NV][NP], g[NV][NP], sq2 = make_float2(0.f, 0.f), dot2 = sq2;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = column(v, 0);
+      if (col < a.width) {
+        read(row, turn, 0, v, col, f[v]);
+        read(row, turn, 1, v, col, g[v]);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          sq2 = fma2(f[v][i], f[v][i], sq2);
+          dot2 = fma2(mul2(g[v][i], w[v][i]), f[v][i], dot2);
+        }
+      }
+    }
+    float sq = warp_sum(sq2.x + sq2.y), dot = warp_sum(dot2.x + dot2.y);
     if ((t & 31) == 0) {
-      buf[turn][0][t >> 5] = sq;
-      buf[turn][1][t >> 5] = dot;
+      buf[side][0][t >> 5] = sq;
+      buf[side][1][t >> 5] = dot;
     }
     __syncthreads();
     sq = dot = 0.f;
 #pragma unroll
     for (int i = 0; i < TPR / 32; ++i) {
-      sq += buf[turn][0][i];
-      dot += buf[turn][1][i];
+      sq += buf[side][0][i];
+      dot += buf[side][1][i];
     }
+    // dx = rho (dy w - s rho c) + ds with c = mean(dy w z) = rho dot / width
     const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
-    const float c = rho * dot / (float)a.width;
+    const float k = -(rho * dot / (float)a.width) * rho * rho;
+    const float2 rho2 = make_float2(rho, rho), k2 = make_float2(k, k);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * TPR + t) * VEC;
+      const int col = column(v, 0);
       if (col < a.width) {
-        float d[VEC];
+        float2 e[NP];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float z = raw_at(cur.s[v], i) * rho, g = raw_at(cur.dy[v], i);
-          acc[v][i] = fmaf(g, z, acc[v][i]);
-          d[i] = rho * (g * w[v][i] - z * c);
-          if (a.ds) d[i] += raw_at(cur.ds[v], i);
+        for (int i = 0; i < NP; ++i) e[i] = make_float2(0.f, 0.f);
+        if (a.ds) read(row, turn, 2, v, col, e);
+        float d[2 * NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          acc[v][i] = fma2(g[v][i], mul2(f[v][i], rho2), acc[v][i]);
+          const float2 x = fma2(f[v][i], k2, fma2(mul2(g[v][i], w[v][i]), rho2, e[i]));
+          d[2 * i] = x.x;
+          d[2 * i + 1] = x.y;
         }
-        if (a.dx) store_vec<VEC, T>(reinterpret_cast<T*>(a.dx) + row * a.ld_dx + col, d);
+        if (a.dx) {
+          T* p = reinterpret_cast<T*>(a.dx) + row * a.ld_dx + col;
+          if constexpr (VEC == 1) {
+            p[0] = from_f<T>(d[0]);
+            if (col + TPR < a.width) p[TPR] = from_f<T>(d[1]);
+          } else {
+            store_vec<VEC, T>(p, d);
+          }
+        }
       }
     }
-    cur = next;
+    if (++turn > kGradAhead) turn = 0;
   }
   if (a.part) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = (v * TPR + t) * VEC;
-      if (col < a.width) {
+    for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) a.part[(size_t)blockIdx.x * a.width + col + i] = acc[v][i];
-      }
-    }
+      for (int i = 0; i < E; ++i)
+        if (column(v, i) < a.width) a.part[(size_t)blockIdx.x * a.width + column(v, i)] = i & 1 ? acc[v][i >> 1].y : acc[v][i >> 1].x;
   }
 }
 
@@ -714,11 +809,11 @@ int grad_blocks(const asd_ops* o, int64_t rows, int width) {
 template <typename T, int VEC>
 void grad_t(const asd_ops* o, const NormGradArgs& n, cudaStream_t st) {
   if (n.width <= 1024)
-    ops_launch(rmsnorm_grad_kernel<T, VEC, 64, 16>, dim3(n.blocks), dim3(64), 0, st, 1, n);
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 64, 16>, dim3(n.blocks), dim3(64), (size_t)grad_smem<T, VEC, 64, 16>, st, 1, n);
   else if (n.width <= 4096)
-    ops_launch(rmsnorm_grad_kernel<T, VEC, 256, 16>, dim3(n.blocks), dim3(256), 0, st, 1, n);
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 256, 16>, dim3(n.blocks), dim3(256), (size_t)grad_smem<T, VEC, 256, 16>, st, 1, n);
   else if (n.width <= kGradWidth)
-    ops_launch(rmsnorm_grad_kernel<T, VEC, 512, 16>, dim3(n.blocks), dim3(512), 0, st, 1, n);
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 512, 16>, dim3(n.blocks), dim3(512), (size_t)grad_smem<T, VEC, 512, 16>, st, 1, n);
   else {
     ops_launch(rmsnorm_grad_long_kernel<T>, dim3(n.rows), dim3(512), 0, st, 1, n);
     if (n.part) ops_launch(columns_dw_kernel<T>, dim3((n.width + 127) / 128, n.blocks), dim3(128), 0, st, 1, n);
@@ -764,8 +859,16 @@ cudaError_t prepare_quantize() {
   return e != cudaSuccess ? e : cudaFuncSetAttribute(quantize_kernel<T, 8, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, quantize_smem<T, 8, 512>);
 }
 }  // namespace
+namespace {
+template <typename T>
+cudaError_t prepare_grad() {
+  const cudaError_t e = cudaFuncSetAttribute(rmsnorm_grad_kernel<T, 8, 256, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, grad_smem<T, 8, 256, 16>);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(rmsnorm_grad_kernel<T, 8, 512, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, grad_smem<T, 8, 512, 16>);
+}
+}  // namespace
 asd_status ops_rows_prepare() {
-  for (cudaError_t e : {prepare_quantize<__half>(), prepare_quantize<__nv_bfloat16>()})
+  for (cudaError_t e : {prepare_quantize<__half>(), prepare_quantize<__nv_bfloat16>(), prepare_grad<float>(), prepare_grad<__half>(),
+                        prepare_grad<__nv_bfloat16>()})
     if (e != cudaSuccess) return ops_fail(ASD_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
   return ASD_OK;
 }
