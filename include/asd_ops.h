@@ -55,7 +55,8 @@ const char* asd_ops_last_error(void);
 /*
  * Every wait inside the matrix kernels is bounded; when its limit (about 0.2 s) runs out the kernel records that
  * and finishes with undefined outputs.  This call synchronises the stream, returns ASD_ERR_TIMEOUT if that has
- * happened on this handle since the last check (and clears it), CUDA if the stream has failed, OK otherwise.
+ * happened on this handle since the last check (and clears it), CUDA if the stream has failed, OK otherwise.  Not to be
+ * called while the stream is being captured.
  */
 asd_status asd_ops_check(asd_ops* ops, void* cuda_stream);
 

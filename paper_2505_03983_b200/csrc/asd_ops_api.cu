@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kMsgBytes = 256;
 thread_local char g_msg[kMsgBytes] = "";
+thread_local cudaError_t g_launch = cudaSuccess;
 
 bool is_type(int t) { return t == ASD_TYPE_F32 || t == ASD_TYPE_F16 || t == ASD_TYPE_BF16; }
 bool off_element(const void* p, int es) { return (uintptr_t)p % (uintptr_t)es != 0; }
@@ -259,8 +260,14 @@ asd_status ops_fail(asd_status st, const char* fmt, ...) {
   va_end(ap);
   return st;
 }
+void ops_note_launch(cudaError_t e) {
+  if (e == cudaSuccess) return;
+  cudaGetLastError();
+  if (g_launch == cudaSuccess) g_launch = e;
+}
 asd_status ops_launched(const char* what) {
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = g_launch;
+  g_launch = cudaSuccess;
   return e == cudaSuccess ? ASD_OK : ops_fail(ASD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 int ops_type_size(int type) { return type == ASD_TYPE_F32 ? 4 : is_type(type) ? 2 : 0; }

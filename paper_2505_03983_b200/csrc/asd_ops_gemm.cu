@@ -588,7 +588,7 @@ int64_t gated_kept_bytes(int64_t rows, int64_t hidden) { return (rows + 31) / 32
 namespace {
 // Whether a product is better split than tiled; `plan` is how.
 bool better_split(const asd_ops* o, const OpsGemm& q, bool early, SplitPlan* plan) {
-  if (q.a[0].mn) return false;
+  if (q.a[0].mn || q.m > kSplitMostRows) return false;
   *plan = plan_split(o, q, early);
   return plan->clocks < std::min(list_clocks(o, &q, 1, 256), list_clocks(o, &q, 1, 128));
 }

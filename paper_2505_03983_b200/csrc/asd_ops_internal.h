@@ -22,7 +22,8 @@ constexpr int kOpsMaxDim = 1 << 24;  // rows' lengths; keeps a row's products of
 constexpr int kOpsMaxK8 = 131071;    // 2^31 / 128^2: the longest sum of 8-bit products that int32 holds
 
 asd_status ops_fail(asd_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-asd_status ops_launched(const char* what);  // OK, or CUDA with the launch's error
+void ops_note_launch(cudaError_t e);        // what a launch returned, kept until ops_launched
+asd_status ops_launched(const char* what);  // OK, or CUDA with the first error of this thread's launches since the last call
 int ops_type_size(int type);                // bytes of an asd_type, 0 if it is none
 
 // Launch with programmatic stream serialization: the kernel may start while its predecessor in the stream ends; every
@@ -45,7 +46,7 @@ inline void ops_launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem,
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.numAttrs = 2;
   }
-  cudaLaunchKernelEx(&cfg, kernel, P(args)...);  // its status is read by ops_launched
+  ops_note_launch(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
 }
 
 // A matrix operand: `rows` rows of `cols` contiguous elements, `ld` elements apart.
@@ -112,6 +113,7 @@ struct SplitPlan {
   int nb, split, stages;  // rows of a CTA, CTAs that share a sum, stages of its operands
   double clocks;          // estimate
 };
+constexpr int64_t kSplitMostRows = 16384;  // beyond, tiles of whole waves are enough
 SplitPlan plan_split(const asd_ops* o, const OpsGemm& g, bool early);
 asd_status ops_split_prepare();
 asd_status ops_gemm_split(const asd_ops* o, const OpsGemm& g, const SplitPlan& p, bool early, cudaStream_t st);

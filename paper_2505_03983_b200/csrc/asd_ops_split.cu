@@ -165,6 +165,7 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
   } else if (warp == 1) {
     // ---------------- MMA issuer ----------------
     if (lane == 0) {
+      if (g.early) grid_dependency_wait();  // the limits of the waits below do not run while the previous kernel does
       const uint64_t step_w = desc_step(g.w_mn);
       int stage = 0;
       uint32_t phase = 0;
@@ -191,8 +192,8 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
     // ---- park this rank's partial sums as part[row][column] ----
     const int quarter = warp & 3, half = (warp - kEpiWarp0) >> 2;  // the two warps of a lane quarter take alternate groups of 16 rows
     const int feat = quarter * 32 + lane;
+    if (g.early) grid_dependency_wait();
     if (I8) {
-      if (g.early) grid_dependency_wait();
       for (int r = (int)threadIdx.x - 64; r < min(g.nb, g.m - row0); r += 256) row_scale[r] = g.scale_a[row0 + r];
     }
     mbar_wait(accf_bar, 0u, dead, g.err);
@@ -218,7 +219,6 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
   if (g.early) grid_launch_dependents();  // after the wait above: what the next one may read early is then complete
 
   if (warp >= kEpiWarp0) {
-    if (g.early) grid_dependency_wait();  // what is stored below may still be in use by an earlier kernel
     // a thread adds up and stores four neighbouring columns, a warp whole rows of the tile
     const int tid = (int)threadIdx.x - 64;
     constexpr int kAcross = F / 4, kRows = 256 / kAcross;  // threads to a row, rows side by side
