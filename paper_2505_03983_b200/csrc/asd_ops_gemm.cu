@@ -71,11 +71,12 @@ struct PairArgs {
 template <int EPI>
 constexpr int products_of = EPI == OPS_STORE ? kMostProducts : 1;
 
-template <int BN, int EPI>
+template <int BN>
 struct OpPairCfg {
   static constexpr int kStageBytes = (BM + BN / 2) * 128;  // per CTA: 128 rows of A, BN / 2 of B, 128 bytes each
-  static constexpr int kBufs = EPI == OPS_GATE_GRAD ? 2 : 1;  // staging buffers of a warp
-  static constexpr int kStages = BN == 256 ? (EPI == OPS_GATE_GRAD ? 5 : 6) : (EPI == OPS_GATE_GRAD ? 6 : 8);
+  static constexpr int kBufs = 2;  // staging buffers of a warp: one is filled while the other's store reads it
+  // 4, 5 and 6 stages of 256 columns take the same time (8192 x 2048 x 8192: 386, 380 and 380 thousand clocks)
+  static constexpr int kStages = BN == 256 ? 5 : 6;
   static constexpr int kTmemCols = 2 * BN;
   static constexpr int kSmemBytes = kStages * kStageBytes + kPairEpiWarps * kBufs * kStoreBytes + 1024 + 256;
   static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
@@ -86,7 +87,8 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
                : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -95,30 +97,51 @@ __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy
 __device__ __forceinline__ void stage_put(uint8_t* buf, int lane, int i, uint4 v) {
   *reinterpret_cast<uint4*>(buf + lane * 128 + ((i ^ (lane & 7)) << 4)) = v;
 }
-// The buffer may be written again: the store that was issued from it has read it.
-__device__ __forceinline__ void stage_free(int lane) {
-  if (lane == 0) bulk_wait_read();
-  __syncwarp();
-}
-__device__ __forceinline__ void stage_send(const CUtensorMap* map, uint32_t buf, int lane, int x, int y, bool any) {
-  fence_async_shared();
-  __syncwarp();
-  if (lane == 0 && any) {
-    tma_store_2d(map, buf, x, y);
-    bulk_commit();
+// A warp's two buffers.  They change places whenever a store is issued from one, so that all but the last store have read
+// theirs when the other is needed again.
+struct Staging {
+  uint8_t* first;
+  uint32_t first_addr;
+  int lane, cur;
+  __device__ __forceinline__ uint8_t* buf() const { return first + cur * kStoreBytes; }
+  __device__ __forceinline__ uint32_t addr() const { return first_addr + cur * kStoreBytes; }
+  // The current buffer may be written (LEFT = 0: both).
+  template <int LEFT = 1>
+  __device__ __forceinline__ void free() const {
+    if (lane == 0) bulk_wait_read<LEFT>();
+    __syncwarp();
   }
-}
-// The staged rows element by element, for outputs that the TMA cannot address: 32 lanes on 32 neighbouring columns.
+  __device__ __forceinline__ void send(const CUtensorMap* map, int x, int y, bool any) {
+    fence_async_shared();
+    __syncwarp();
+    if (!any) return;
+    if (lane == 0) {
+      tma_store_2d(map, addr(), x, y);
+      bulk_commit();
+    }
+    cur ^= 1;
+  }
+};
+// The staged rows for outputs that the TMA cannot address: a row at a time, 64 columns in 32 words.  Where a row starts in
+// the middle of a word its first and its last element go alone, and lane i takes columns 2 i - 1 and 2 i.
 __device__ __forceinline__ void rows_out16(const uint8_t* buf, void* c, int64_t ldc, int lane, int row0, int col0, int m, int n) {
   __syncwarp();
   uint16_t* p = reinterpret_cast<uint16_t*>(c) + row0 * ldc + col0;
-  const int rows = min(32, m - row0);
+  const int rows = min(32, m - row0), cols = min(64, n - col0);
+  if (cols <= 0) return;
+#pragma unroll 8
   for (int r = 0; r < rows; ++r, p += ldc) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int i = 32 * h + lane;
-      if (col0 + i < n) p[i] = *reinterpret_cast<const uint16_t*>(buf + r * 128 + (((i >> 3) ^ (r & 7)) << 4) + 2 * (i & 7));
-    }
+    auto at = [&](int i) { return (uint32_t)*reinterpret_cast<const uint16_t*>(buf + r * 128 + (((i >> 3) ^ (r & 7)) << 4) + 2 * (i & 7)); };
+    const int off = (int)(((uintptr_t)p >> 1) & 1);
+    const int i = 2 * lane - off, j = i + 1;
+    const uint32_t lo = at(max(i, 0)), hi = at(j);
+    if (i >= 0 && j < cols)
+      *reinterpret_cast<uint32_t*>(p + i) = lo | (hi << 16);
+    else if (i >= 0 && i < cols)
+      p[i] = (uint16_t)lo;
+    else if (i < 0)
+      p[0] = (uint16_t)hi;
+    if (off && lane == 31 && cols == 64) p[63] = (uint16_t)at(63);
   }
   __syncwarp();
 }
@@ -126,6 +149,7 @@ __device__ __forceinline__ void rows_out32(const uint8_t* buf, void* c, int64_t 
   __syncwarp();
   uint32_t* p = reinterpret_cast<uint32_t*>(c) + row0 * ldc + col0;
   const int rows = min(32, m - row0);
+#pragma unroll 8
   for (int r = 0; r < rows; ++r, p += ldc)
     if (col0 + lane < n) p[lane] = *reinterpret_cast<const uint32_t*>(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + 4 * (lane & 3));
   __syncwarp();
@@ -156,7 +180,7 @@ __device__ __forceinline__ Tile tile_at(const PairArgs<N>& g, int t) {
 template <int BN, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __grid_constant__ PairArgs<products_of<EPI>> g) {
-  using C = OpPairCfg<BN, EPI>;
+  using C = OpPairCfg<BN>;
   constexpr int S = C::kStages;
   constexpr bool I8 = EPI == OPS_I8;
   // columns of C to a tile: half of the accumulator's where it holds g and u
@@ -294,8 +318,9 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
     const int half = (warp - kEpiWarp0) >> 2;  // of the tile's columns
     const bool f16 = g.out_type == ASD_TYPE_F16;
     const bool gelu = g.gelu != 0;
-    uint8_t* buf = stage_ptr + (warp - kEpiWarp0) * C::kBufs * kStoreBytes;
-    const uint32_t buf_addr = smem_u32(buf);
+    const bool scales_wide = (((uintptr_t)g.scale_b | (uintptr_t)g.bias) & 15) == 0;
+    uint8_t* const bufs = stage_ptr + (warp - kEpiWarp0) * C::kBufs * kStoreBytes;
+    Staging out{bufs, smem_u32(bufs), lane, 0};
     constexpr int kUnits = CN / 64;  // of 64 columns; a tile of one is the first four warps'
     constexpr int kMine = kUnits >= 2 ? kUnits / 2 : 1;
     int it = 0;
@@ -331,7 +356,8 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
           const int col0 = tile.n0 + c0;
           const bool any = rows_any && col0 < n;
           if (EPI == OPS_STORE || EPI == OPS_GATE) {
-            if (tma) stage_free(lane);
+            if (tma) out.free();
+            uint8_t* const buf = out.buf();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               uint32_t w[16];
@@ -380,11 +406,11 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
               stage_half(buf, lane, h, w);
             }
             if (tma)
-              stage_send(&mp.c[0], buf_addr, lane, col0, row0, any);
+              out.send(&mp.c[0], col0, row0, any);
             else
               rows_out16(buf, p.c, p.ldc, lane, row0, col0, m, n);
           } else if (EPI == OPS_GATE_GRAD) {
-            stage_free(lane);
+            out.free<0>();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               uint32_t r[32], wg[16], wu[16];
@@ -397,41 +423,53 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
                 wu[i] = pack16(d0 * kept_value(kept[1], 2 * i), d1 * kept_value(kept[1], 2 * i + 1), f16);
               }
               if (h == 0 || u + 1 < kMine) fetch_kept(col0 + 32 * h + 32);
-              stage_half(buf, lane, h, wg);
-              stage_half(buf + kStoreBytes, lane, h, wu);
+              stage_half(bufs, lane, h, wg);
+              stage_half(bufs + kStoreBytes, lane, h, wu);
             }
             fence_async_shared();
             __syncwarp();
             if (lane == 0 && any) {
-              tma_store_2d(&mp.c[0], buf_addr, col0, row0);
-              tma_store_2d(&mp.c[1], buf_addr + kStoreBytes, col0, row0);
+              tma_store_2d(&mp.c[0], out.first_addr, col0, row0);
+              tma_store_2d(&mp.c[1], out.first_addr + kStoreBytes, col0, row0);
               bulk_commit();
             }
           } else {
             const bool f32 = g.out_type == ASD_TYPE_F32;
-            if (tma) stage_free(lane);
+            if (tma) out.free();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+              uint8_t* const buf = out.buf();
               const int col = col0 + 32 * h;
               uint32_t r[32];
               tc_ld32(t0 + c0 + 32 * h, r);
               tc_wait_ld();
               float f[32];
-              // every lane needs the same columns' scales: one load per lane, handed around
-              const int mine = col + lane;
-              const float sb = mine < n ? g.scale_b[mine] : 0.f;
-              const float bb = g.bias && mine < n ? g.bias[mine] : 0.f;
+              if (col + 32 <= n && scales_wide) {  // every lane the same columns' scales, four at a time
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                f[i] = fmaf((float)(int)r[i] * sa, __shfl_sync(0xffffffffu, sb, i), __shfl_sync(0xffffffffu, bb, i));
+                for (int i = 0; i < 32; i += 4) {
+                  const float4 sb = *reinterpret_cast<const float4*>(g.scale_b + col + i);
+                  const float4 bb = g.bias ? *reinterpret_cast<const float4*>(g.bias + col + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+                  f[i] = fmaf((float)(int)r[i] * sa, sb.x, bb.x);
+                  f[i + 1] = fmaf((float)(int)r[i + 1] * sa, sb.y, bb.y);
+                  f[i + 2] = fmaf((float)(int)r[i + 2] * sa, sb.z, bb.z);
+                  f[i + 3] = fmaf((float)(int)r[i + 3] * sa, sb.w, bb.w);
+                }
+              } else {  // one load per lane, handed around
+                const int mine = col + lane;
+                const float sb = mine < n ? g.scale_b[mine] : 0.f;
+                const float bb = g.bias && mine < n ? g.bias[mine] : 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  f[i] = fmaf((float)(int)r[i] * sa, __shfl_sync(0xffffffffu, sb, i), __shfl_sync(0xffffffffu, bb, i));
+              }
               if (f32) {
-                if (tma && h == 1) stage_free(lane);
+                if (tma && h == 1) out.free();
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                   stage_put(buf, lane, i, make_uint4(__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]),
                                                      __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3])));
                 if (tma)
-                  stage_send(&mp.c[0], buf_addr, lane, col, row0, rows_any && col < n);
+                  out.send(&mp.c[0], col, row0, rows_any && col < n);
                 else
                   rows_out32(buf, p.c, p.ldc, lane, row0, col, m, n);
               } else {
@@ -443,9 +481,9 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
             }
             if (!f32) {
               if (tma)
-                stage_send(&mp.c[0], buf_addr, lane, col0, row0, any);
+                out.send(&mp.c[0], col0, row0, any);
               else
-                rows_out16(buf, p.c, p.ldc, lane, row0, col0, m, n);
+                rows_out16(out.buf(), p.c, p.ldc, lane, row0, col0, m, n);
             }
           }
         }
@@ -496,7 +534,7 @@ namespace {
 
 template <int BN, int EPI>
 asd_status launch_pair(const asd_ops* o, const OpsGemm* list, int count, cudaStream_t st) {
-  using C = OpPairCfg<BN, EPI>;
+  using C = OpPairCfg<BN>;
   constexpr bool I8 = EPI == OPS_I8;
   constexpr int CN = EPI == OPS_GATE ? BN / 2 : BN, N = products_of<EPI>;
   PairMaps<N> maps;
@@ -578,7 +616,7 @@ asd_status launch_width(const asd_ops* o, const OpsGemm* list, int count, cudaSt
 
 template <int BN, int EPI>
 cudaError_t prepare_pair() {
-  return cudaFuncSetAttribute(op_pair_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, OpPairCfg<BN, EPI>::kSmemBytes);
+  return cudaFuncSetAttribute(op_pair_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, OpPairCfg<BN>::kSmemBytes);
 }
 
 }  // namespace
