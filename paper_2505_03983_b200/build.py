@@ -45,6 +45,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     deps = srcs + [os.path.join(HERE, "csrc", "asd_internal.h"), os.path.join(HERE, "csrc", "asd_device.cuh"),
                    os.path.join(HERE, "csrc", "asd_tc.cuh"),
                    os.path.join(HERE, "csrc", "asd_ops_internal.h"), os.path.join(HERE, "csrc", "asd_ops_tc.cuh"),
+                   os.path.join(HERE, "csrc", "asd_ops_act.cuh"),
                    os.path.join(ROOT, "include", "asd.h"), os.path.join(ROOT, "include", "asd_ops.h")]
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(deps):
         _build_torch_binding(force)

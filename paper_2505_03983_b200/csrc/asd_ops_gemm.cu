@@ -373,34 +373,26 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
                 tc_ld32(t0 + c0 + 32 * h, rg);
                 tc_ld32(t0 + CN + c0 + 32 * h, ru);
                 tc_wait_ld();
-                if (g.kept) {
-                  // rg, ru become the factors that are kept
+#pragma unroll
+                for (int q = 0; q < 32; q += 16) {
+                  float gg[16], uu[16], hh[16];
 #pragma unroll
                   for (int i = 0; i < 16; ++i) {
-                    float h2[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                      const float v = __uint_as_float(ru[2 * i + e]);
-                      float a, da;
-                      gate_grad(__uint_as_float(rg[2 * i + e]), gelu, a, da);
-                      h2[e] = a * v;
-                      rg[2 * i + e] = __float_as_uint(v * da);
-                      ru[2 * i + e] = __float_as_uint(a);
-                    }
-                    w[i] = pack16(h2[0], h2[1], f16);
+                    gg[i] = __uint_as_float(rg[q + i]);
+                    uu[i] = __uint_as_float(ru[q + i]);
                   }
-                  if (rows_any && col < n) {
-                    uint8_t* b = g.kept + kept_offset(row0, col, g.kept_cols);
-                    kept_store(b, lane, rg);
-                    kept_store(b + kKeptHalf, lane, ru);
-                  }
-                } else {
+                  gated(gg, uu, hh, gelu, g.kept != nullptr);
 #pragma unroll
                   for (int i = 0; i < 16; ++i) {
-                    const float h0 = gate_value(__uint_as_float(rg[2 * i]), gelu) * __uint_as_float(ru[2 * i]);
-                    const float h1 = gate_value(__uint_as_float(rg[2 * i + 1]), gelu) * __uint_as_float(ru[2 * i + 1]);
-                    w[i] = pack16(h0, h1, f16);
+                    rg[q + i] = __float_as_uint(gg[i]);
+                    ru[q + i] = __float_as_uint(uu[i]);
+                    if (i & 1) w[(q + i) >> 1] = pack16(hh[i - 1], hh[i], f16);
                   }
+                }
+                if (g.kept && rows_any && col < n) {
+                  uint8_t* b = g.kept + kept_offset(row0, col, g.kept_cols);
+                  kept_store(b, lane, rg);
+                  kept_store(b + kKeptHalf, lane, ru);
                 }
               }
               stage_half(buf, lane, h, w);

@@ -8,6 +8,7 @@
 // multiple of 8 elements is read element by element, neighbouring threads on neighbouring elements.
 #include <type_traits>
 
+#include "asd_ops_act.cuh"
 #include "asd_ops_internal.h"
 
 namespace asd {
@@ -158,7 +159,7 @@ __device__ __forceinline__ float act_value(float g, int act) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(1.f + e));
     return g * p;
   }
-  return 0.5f * g * (1.f + erff(g * 0.7071067811865476f));
+  return g * normal_cdf(g).x;
 }
 
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {

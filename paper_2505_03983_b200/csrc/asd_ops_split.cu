@@ -261,23 +261,18 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
         for (int i = 0; i < R; ++i) {
           const int row = row0 + lr0 + i * kRows * g.split;
           if (row >= row0 + m) break;
-          const float y[4] = {__uint_as_float(v[i].x), __uint_as_float(v[i].y), __uint_as_float(v[i].z), __uint_as_float(v[i].w)};
+          float y[4] = {__uint_as_float(v[i].x), __uint_as_float(v[i].y), __uint_as_float(v[i].z), __uint_as_float(v[i].w)};
           const int64_t at = row * g.ldc + col;
           if (EPI == OPS_STORE) {
             store4(g.c[0], at, y, cols, g.wide, f16);
           } else if (EPI == OPS_GATE) {
-            const float w[4] = {__uint_as_float(u[i].x), __uint_as_float(u[i].y), __uint_as_float(u[i].z), __uint_as_float(u[i].w)};
-            float a[4], d[4], h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              gate_grad(y[e], gelu, a[e], d[e]);
-              h[e] = a[e] * w[e];
-              d[e] *= w[e];
-            }
+            float w[4] = {__uint_as_float(u[i].x), __uint_as_float(u[i].y), __uint_as_float(u[i].z), __uint_as_float(u[i].w)};
+            float h[4];
+            gated(y, w, h, gelu, g.kept != nullptr);
             if (g.kept) {
               uint8_t* b = g.kept + kept_offset(row, col, g.kept_cols);
-              kept_put4(b, row & 31, col & 31, d);
-              kept_put4(b + kKeptHalf, row & 31, col & 31, a);
+              kept_put4(b, row & 31, col & 31, y);
+              kept_put4(b + kKeptHalf, row & 31, col & 31, w);
             }
             store4(g.c[0], at, h, cols, g.wide, f16);
           } else if (EPI == OPS_GATE_GRAD) {

@@ -179,14 +179,14 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
         if (EPI == OPS_GATE) u += __uint_as_float(sums[w * of_warp + 8]);
       }
       if (EPI == OPS_GATE) {
-        float act, slope;
-        gate_grad(v, a.gelu != 0, act, slope);
+        float g1[1] = {v}, u1[1] = {u}, h1[1];
+        gated(g1, u1, h1, a.gelu != 0, a.kept != nullptr);
         if (a.kept) {
           uint8_t* b = a.kept + kept_offset(row, col, a.kept_cols);
-          kept_put(b, row, col & 31, u * slope);
-          kept_put(b + kKeptHalf, row, col & 31, act);
+          kept_put(b, row, col & 31, g1[0]);
+          kept_put(b + kKeptHalf, row, col & 31, u1[0]);
         }
-        v = act * u;
+        v = h1[0];
       }
       reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(v, KIND == KIND_F16);
     }

@@ -3,6 +3,7 @@
 // the two projections.  Everything here has internal linkage.
 #pragma once
 
+#include "asd_ops_act.cuh"
 #include "asd_ops_internal.h"
 #include "asd_tc.cuh"
 
@@ -60,21 +61,48 @@ __device__ __forceinline__ uint16_t round16(float a, bool f16) {
 // act(g).  The exponential and reciprocal are the approximate instructions (relative error some 2^-22, far below the
 // 16-bit rounding that follows).
 __device__ __forceinline__ float sigmoid_approx(float g) { return rcp_approx(1.f + ex2_approx(g * kNegLog2e)); }
-__device__ __forceinline__ float gate_value(float g, bool gelu) {
-  if (!gelu) return g * sigmoid_approx(g);
-  return 0.5f * g * (1.f + erff(g * 0.7071067811865476f));
+template <bool GELU>
+__device__ __forceinline__ float gate_value(float g) {
+  return g * (GELU ? normal_cdf(g).x : sigmoid_approx(g));
 }
 // act(g) and act'(g):  silu' = p (1 + g (1 - p)),  gelu' = Phi + g phi.
-__device__ __forceinline__ void gate_grad(float g, bool gelu, float& a, float& da) {
-  if (!gelu) {
+template <bool GELU>
+__device__ __forceinline__ void gate_grad(float g, float& a, float& da) {
+  if (!GELU) {
     const float p = sigmoid_approx(g);
     a = g * p;
     da = fmaf(a, 1.f - p, p);
   } else {
-    const float p = 0.5f * (1.f + erff(g * 0.7071067811865476f));
-    a = g * p;
-    da = fmaf(g * 0.3989422804014327f, ex2_approx(g * g * -0.7213475204444817f), p);
+    const float2 p = normal_cdf(g);
+    a = g * p.x;
+    da = fmaf(g * 0.3989422804014327f, p.y, p.x);
   }
+}
+
+// N gated values: h = act(g) u, and (KEEP) g and u replaced by u act'(g) and act(g).  The activation is chosen once for all of
+// them: a branch for each would keep the elements from being worked on side by side (a 256 x 128 tile of h: 11 against 4
+// thousand clocks).
+template <bool GELU, bool KEEP, int N>
+__device__ __forceinline__ void gated_n(float (&g)[N], float (&u)[N], float (&h)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (KEEP) {
+      float a, da;
+      gate_grad<GELU>(g[i], a, da);
+      h[i] = a * u[i];
+      g[i] = u[i] * da;
+      u[i] = a;
+    } else {
+      h[i] = gate_value<GELU>(g[i]) * u[i];
+    }
+  }
+}
+template <int N>
+__device__ __forceinline__ void gated(float (&g)[N], float (&u)[N], float (&h)[N], bool gelu, bool keep) {
+  if (gelu)
+    keep ? gated_n<true, true>(g, u, h) : gated_n<true, false>(g, u, h);
+  else
+    keep ? gated_n<false, true>(g, u, h) : gated_n<false, false>(g, u, h);
 }
 
 // What a training step keeps of the gate.  h = act(g) u has the derivatives act(g) in u and u act'(g) in g, and it is these
