@@ -4,8 +4,10 @@
 //
 // All of them are bound by memory: a row is read once, kept in registers over its reductions, and written once.  A row
 // belongs to 32, 128, 256 or 512 threads (rows of up to 1024, 4096, 8192, 16384), 32 elements to a thread, so that a thread has its
-// 16-byte loads in flight together; longer rows are read a second time.  A row whose address, distance or length is not a
-// multiple of 8 elements is read element by element, neighbouring threads on neighbouring elements.
+// 16-byte loads in flight together; longer rows are read a second time.  Rows whose address, distance or length is not a
+// multiple of 8 elements come into shared memory in the aligned 16-byte pieces that hold them, one row ahead, and are read
+// from there element by element, neighbouring threads on neighbouring elements (read so from memory, 6001 rows of 2 x 2477
+// bf16 took 127 us to quantise).
 #include <type_traits>
 
 #include "asd_ops_act.cuh"
@@ -16,6 +18,7 @@ namespace {
 
 constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: the least magnitude that a row's scale is made from
 constexpr int kPer = 32;                         // elements of a row that one thread keeps
+constexpr int kStagedSmem = 220 * 1024;          // shared memory for staged rows
 
 __device__ __forceinline__ void dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -208,6 +211,132 @@ struct NormArgs {
 template <int TPR>
 constexpr int block_of = TPR == 32 ? 128 : TPR;
 
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A row of `bytes` into shared memory by T threads, in aligned pieces; it starts (address & 15) bytes into dst.  Nothing
+// beyond the row's end is read; before its start, the rest of the piece that holds it.
+__device__ __forceinline__ void stage_row(uint8_t* dst, const void* src, int bytes, int t, int T) {
+  const uint8_t* p = reinterpret_cast<const uint8_t*>((uintptr_t)src & ~(uintptr_t)15);
+  const int end = bytes + (int)((uintptr_t)src & 15);
+  for (int at = 16 * t; at < end; at += 16 * T)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + at)), "l"(p + at), "r"(min(16, end - at))
+                 : "memory");
+}
+template <typename T>
+__device__ __forceinline__ const T* staged(const uint8_t* dst, const void* src) {
+  return reinterpret_cast<const T*>(dst + ((uintptr_t)src & 15));
+}
+__host__ __device__ inline int stage_pitch(int64_t bytes) { return (int)((bytes + 15 + 15) / 16 * 16); }
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+// The threads of a row.
+template <int TPR>
+__device__ __forceinline__ void row_sync() {
+  if (TPR == 32)
+    __syncwarp();
+  else
+    __syncthreads();
+}
+// How rows that are staged are walked over: `stride` rows side by side, each with `ahead` + 1 buffers of `pitch` bytes for each
+// of its `parts`.
+struct Walk {
+  int stride, ahead, pitch, parts;
+};
+// Calls work(row, turn) for each of a row slot's rows with the row in the buffers of `turn`; fetch(row, turn) copies one.  The
+// work has to read its buffers before a barrier of the row's threads that it takes itself.
+template <int TPR, typename F, typename W>
+__device__ __forceinline__ void walk_rows(int first, int rows, const Walk& k, F fetch, W work) {
+  if (k.ahead) {
+    if (first < rows) fetch(first, 0);
+    commit_copies();
+  }
+  int turn = 0;
+  for (int64_t row = first; row < rows; row += k.stride) {
+    if (k.ahead) {
+      if (row + k.stride < rows) fetch((int)(row + k.stride), turn ^ 1);
+      commit_copies();
+      wait_copies<1>();
+    } else {
+      fetch((int)row, 0);
+      commit_copies();
+      wait_copies<0>();
+    }
+    row_sync<TPR>();  // every thread's copies are in place
+    work((int)row, turn);
+    turn ^= k.ahead;
+  }
+}
+
+// s and its norm for staged rows.
+template <typename T, int TPR, bool Q8>
+__global__ void __launch_bounds__(block_of<TPR>) rmsnorm_staged_kernel(const NormArgs a, const Walk k) {
+  extern __shared__ __align__(16) uint8_t rows_smem[];
+  __shared__ float buf_s[2][TPR / 32];
+  __shared__ uint32_t buf_m[2][TPR / 32];
+  dep_wait();
+  dep_launch();
+  const int t = TPR == 32 ? (threadIdx.x & 31) : threadIdx.x, slot = TPR == 32 ? threadIdx.x >> 5 : 0;
+  uint8_t* mine = rows_smem + slot * (k.ahead + 1) * k.parts * k.pitch;
+  auto buffer = [&](int turn, int part) { return mine + (turn * k.parts + part) * k.pitch; };
+  auto xrow = [&](int row) { return reinterpret_cast<const T*>(a.x) + row * a.ld_x; };
+  auto rrow = [&](int row) { return reinterpret_cast<const T*>(a.r) + row * a.ld_r; };
+  const int n = (a.width - t + TPR - 1) / TPR;  // this thread's elements t, t + TPR, ...
+  int side = 0;
+  walk_rows<TPR>(
+      TPR == 32 ? blockIdx.x * 4 + slot : blockIdx.x, a.rows, k,
+      [&](int row, int turn) {
+        stage_row(buffer(turn, 0), xrow(row), a.width * (int)sizeof(T), t, TPR);
+        if (a.r) stage_row(buffer(turn, 1), rrow(row), a.width * (int)sizeof(T), t, TPR);
+      },
+      [&](int row, int turn) {
+        const T* x = staged<T>(buffer(turn, 0), xrow(row)) + t;
+        const T* r = a.r ? staged<T>(buffer(turn, 1), rrow(row)) + t : nullptr;
+        T* so = a.sum ? reinterpret_cast<T*>(a.sum) + row * a.ld_s + t : nullptr;
+        float f[kPer], sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          f[i] = 0.f;
+          if (i < n) {
+            T v = x[i * TPR];
+            if (r) v = from_f<T>(to_f<T>(v) + to_f<T>(r[i * TPR]));
+            if (so) so[i * TPR] = v;
+            f[i] = to_f<T>(v);
+            sq = fmaf(f[i], f[i], sq);
+          }
+        }
+        sq = row_sum<TPR>(sq, buf_s[side]);
+        const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
+        uint32_t most = 0;
+        T* y = reinterpret_cast<T*>(a.y) + row * a.ld_y + t;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          if (i < n) {
+            float w[1];
+            load_weight<1, T>(a.w, a.w_f32, t + i * TPR, w);
+            f[i] = f[i] * rho * w[0];
+            if (Q8)
+              most = max(most, mag(f[i]));
+            else
+              y[i * TPR] = from_f<T>(f[i]);
+          }
+        }
+        if (Q8) {
+          const RowScale rs = row_scale(row_max<TPR>(most, buf_m[side]));
+          int8_t* q = reinterpret_cast<int8_t*>(a.y) + row * a.ld_y + t;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i)
+            if (i < n) q[i * TPR] = rs.ok ? (int8_t)rounded_bits(f[i], rs.inv) : (int8_t)0;
+          if (t == 0) a.scale[row] = rs.scale;
+        }
+        side ^= 1;
+      });
+}
+
 // s and its norm.  TPR threads to a row, kPer elements each (LONG: any number, s read back or added up again for the
 // second pass).
 template <typename T, int VEC, int TPR, bool Q8, bool LONG>
@@ -349,10 +478,6 @@ struct QuantArgs {
   int64_t ld_x, ld_q;
 };
 
-__device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-
 // A row's threads walk over rows.  With the gate, 16-bit rows that can be read in 16-byte pieces come through shared memory
 // one row ahead (cp.async; a thread reads back only what it has copied itself, so that takes no barrier): two transcendental
 // instructions an element and the barrier of the row's maximum would leave memory idle otherwise.
@@ -436,6 +561,50 @@ __global__ void __launch_bounds__(block_of<TPR>) quantize_kernel(const QuantArgs
   }
 }
 
+// The same for staged rows.
+template <typename T, int TPR>
+__global__ void __launch_bounds__(block_of<TPR>) quantize_staged_kernel(const QuantArgs a, const Walk k) {
+  extern __shared__ __align__(16) uint8_t rows_smem[];
+  __shared__ uint32_t buf_m[2][TPR / 32];
+  dep_wait();
+  dep_launch();
+  const int t = TPR == 32 ? (threadIdx.x & 31) : threadIdx.x, slot = TPR == 32 ? threadIdx.x >> 5 : 0;
+  uint8_t* mine = rows_smem + slot * (k.ahead + 1) * k.pitch;
+  const bool gate = a.act != ASD_ACT_NONE;
+  auto xrow = [&](int row) { return reinterpret_cast<const T*>(a.x) + row * a.ld_x; };
+  const int n = (a.width - t + TPR - 1) / TPR;
+  int side = 0;
+  walk_rows<TPR>(
+      TPR == 32 ? blockIdx.x * 4 + slot : blockIdx.x, a.rows, k,
+      [&](int row, int turn) { stage_row(mine + turn * k.pitch, xrow(row), (gate ? 2 : 1) * a.width * (int)sizeof(T), t, TPR); },
+      [&](int row, int turn) {
+        const T* x = staged<T>(mine + turn * k.pitch, xrow(row)) + t;
+        float f[kPer];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; i += 2) {
+          float2 g = make_float2(0.f, 0.f), u = g;
+          if (i < n) g.x = to_f<T>(x[i * TPR]);
+          if (i + 1 < n) g.y = to_f<T>(x[(i + 1) * TPR]);
+          if (gate) {
+            if (i < n) u.x = to_f<T>(x[a.width + i * TPR]);
+            if (i + 1 < n) u.y = to_f<T>(x[a.width + (i + 1) * TPR]);
+            g = gated2(g, u, a.act);
+          }
+          f[i] = g.x;
+          f[i + 1] = g.y;
+          most = max(most, max(mag(g.x), mag(g.y)));
+        }
+        const RowScale rs = row_scale(row_max<TPR>(most, buf_m[side]));
+        int8_t* q = a.q + row * a.ld_q + t;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (i < n) q[i * TPR] = rs.ok ? (int8_t)rounded_bits(f[i], rs.inv) : (int8_t)0;
+        if (t == 0) a.scale[row] = rs.scale;
+        side ^= 1;
+      });
+}
+
 // Rows of more than 16384, read twice.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(512) quantize_long_kernel(const QuantArgs a) {
@@ -473,6 +642,7 @@ __global__ void __launch_bounds__(512) quantize_long_kernel(const QuantArgs a) {
 
 struct NormGradArgs {
   int rows, width, w_f32, blocks;
+  int pitch;    // of a staged row
   float eps;
   const void *dy, *s, *ds, *w;
   void* dx;
@@ -483,9 +653,9 @@ struct NormGradArgs {
 
 // Gradients.  One block walks over rows blockIdx.x, + blocks, ...; a thread keeps the same columns in every row, so the
 // weights and the sums of dw over the block's rows stay in its registers; the sums are written once, to be added up by
-// reduce_dw_kernel.  Both sums of a row, of s^2 and of dy w s, are taken together: mean(dy w z) = rho mean(dy w s).  Rows
-// that can be read in 16-byte pieces come through shared memory two rows ahead (32 bits: one) (cp.async; a thread reads back only
-// what it has copied itself), so that memory is busy over the barriers; the others are read where they are needed.
+// reduce_dw_kernel.  Both sums of a row, of s^2 and of dy w s, are taken together: mean(dy w z) = rho mean(dy w s).  Rows come
+// through shared memory two rows ahead (32 bits: one), so that memory is busy over the barriers: where they can be read in
+// 16-byte pieces a thread reads back only what it has copied itself, the others are staged.
 template <typename T>
 constexpr int grad_ahead = sizeof(T) == 2 ? 2 : 1;
 template <typename T, int VEC, int TPR, int PER>
@@ -525,8 +695,13 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
   const T* base[3] = {reinterpret_cast<const T*>(a.s), reinterpret_cast<const T*>(a.dy), reinterpret_cast<const T*>(a.ds)};
   const int64_t ld[3] = {a.ld_s, a.ld_dy, a.ld_ds};
   auto slot = [&](int turn, int part, int v, int piece) { return ahead + (((turn * 3 + part) * NV + v) * PIECES + piece) * TPR + t; };
+  auto staged_at = [&](int turn, int part) { return reinterpret_cast<uint8_t*>(ahead) + (turn * 3 + part) * a.pitch; };
   auto fetch = [&](int64_t row, int turn) {
-    if (row < a.rows) {
+    if (!AHEAD && row < a.rows) {
+      for (int part = 0; part < 3; ++part)
+        if (part < 2 || a.ds) stage_row(staged_at(turn, part), base[part] + row * ld[part], a.width * (int)sizeof(T), t, TPR);
+    }
+    if (AHEAD && row < a.rows) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int col = column(v, 0);
@@ -541,7 +716,7 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
         }
       }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    commit_copies();
   };
   // VEC elements of s (0), dy (1) or ds (2) of the row that is worked on
   auto read = [&](int64_t row, int turn, int part, int v, int col, float2(&f)[NP]) {
@@ -552,19 +727,23 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
 #pragma unroll
       for (int i = 0; i < NP; ++i) f[i] = unpack<T>(e, i);
     } else {
-      const T* p = base[part] + row * ld[part] + col;
+      const T* p = staged<T>(staged_at(turn, part), base[part] + row * ld[part]) + col;
       f[0] = make_float2(to_f<T>(p[0]), col + TPR < a.width ? to_f<T>(p[TPR]) : 0.f);
     }
   };
-  if (AHEAD) {
 #pragma unroll
-    for (int k = 0; k < kGradAhead; ++k) fetch(blockIdx.x + (int64_t)k * a.blocks, k);
-  }
+  for (int k = 0; k < kGradAhead; ++k) fetch(blockIdx.x + (int64_t)k * a.blocks, k);
   int turn = 0, side = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks, side ^= 1) {
+    const int64_t then = row + (int64_t)kGradAhead * a.blocks;
+    const int free_turn = turn == 0 ? kGradAhead : turn - 1;
     if (AHEAD) {
-      fetch(row + (int64_t)kGradAhead * a.blocks, turn == 0 ? kGradAhead : turn - 1);
-      asm volatile("cp.async.wait_group %0;" ::"n"(kGradAhead) : "memory");
+      fetch(then, free_turn);
+      wait_copies<kGradAhead>();
+    } else {  // a thread reads what others have copied: all copies in place, and the row before no longer read
+      wait_copies<kGradAhead - 1>();
+      __syncthreads();
+      fetch(then, free_turn);
     }
     float2 f[NV][NP], g[NV][NP], sq2 = make_float2(0.f, 0.f), dot2 = sq2;
 #pragma unroll
@@ -753,49 +932,88 @@ int row_threads(const asd_ops* o, int64_t rows, int width) {
   return 512;
 }
 
-template <typename T, int VEC, bool Q8>
-void rmsnorm_t(const asd_ops* o, const NormArgs& n, cudaStream_t st) {
-  const int tpr = row_threads(o, n.rows, n.width);
-  if (tpr == 32)
-    ops_launch(rmsnorm_kernel<T, VEC, 32, Q8, false>, dim3((n.rows + 3) / 4), dim3(128), 0, st, 1, n);
-  else if (tpr == 128)
-    ops_launch(rmsnorm_kernel<T, VEC, 128, Q8, false>, dim3(n.rows), dim3(128), 0, st, 1, n);
-  else if (tpr == 256)
-    ops_launch(rmsnorm_kernel<T, VEC, 256, Q8, false>, dim3(n.rows), dim3(256), 0, st, 1, n);
-  else if (n.width <= 512 * kPer)
-    ops_launch(rmsnorm_kernel<T, VEC, 512, Q8, false>, dim3(n.rows), dim3(512), 0, st, 1, n);
-  else
-    ops_launch(rmsnorm_kernel<T, VEC, 512, Q8, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
+// How staged rows of `parts` operands of `bytes` are walked over by blocks of `threads` with `slots` rows each: one row ahead
+// where its buffers fit, and as many blocks as the SMs hold together.
+struct WalkPlan {
+  Walk k;
+  int grid, smem;
+};
+WalkPlan plan_walk(const asd_ops* o, int rows, int64_t bytes, int parts, int slots, int threads) {
+  WalkPlan p;
+  p.k.pitch = stage_pitch(bytes);
+  p.k.parts = parts;
+  p.k.ahead = 2 * slots * parts * p.k.pitch <= kStagedSmem ? 1 : 0;
+  p.smem = (p.k.ahead + 1) * slots * parts * p.k.pitch;
+  int side = kStagedSmem / p.smem;
+  if (side > 1024 / threads) side = 1024 / threads;
+  const int blocks = (rows + slots - 1) / slots, most = o->num_sms * (side < 1 ? 1 : side);
+  p.grid = blocks < most ? blocks : most;
+  p.k.stride = p.grid * slots;
+  return p;
+}
+template <typename T, int TPR, bool Q8>
+void rmsnorm_staged(const asd_ops* o, const NormArgs& n, cudaStream_t st) {
+  const WalkPlan p = plan_walk(o, n.rows, (int64_t)n.width * sizeof(T), n.r ? 2 : 1, TPR == 32 ? 4 : 1, block_of<TPR>);
+  ops_launch(rmsnorm_staged_kernel<T, TPR, Q8>, dim3(p.grid), dim3(block_of<TPR>), (size_t)p.smem, st, 1, n, p.k);
+}
+template <typename T, bool Q8>
+void rmsnorm_t(const asd_ops* o, const NormArgs& n, bool vec, cudaStream_t st) {
+  if (n.width > 512 * kPer) {
+    if (vec)
+      ops_launch(rmsnorm_kernel<T, 8, 512, Q8, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    else
+      ops_launch(rmsnorm_kernel<T, 1, 512, Q8, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    return;
+  }
+  switch (row_threads(o, n.rows, n.width)) {
+    case 32:
+      if (!vec) return rmsnorm_staged<T, 32, Q8>(o, n, st);
+      return ops_launch(rmsnorm_kernel<T, 8, 32, Q8, false>, dim3((n.rows + 3) / 4), dim3(128), 0, st, 1, n);
+    case 128:
+      if (!vec) return rmsnorm_staged<T, 128, Q8>(o, n, st);
+      return ops_launch(rmsnorm_kernel<T, 8, 128, Q8, false>, dim3(n.rows), dim3(128), 0, st, 1, n);
+    case 256:
+      if (!vec) return rmsnorm_staged<T, 256, Q8>(o, n, st);
+      return ops_launch(rmsnorm_kernel<T, 8, 256, Q8, false>, dim3(n.rows), dim3(256), 0, st, 1, n);
+    default:
+      if (!vec) return rmsnorm_staged<T, 512, Q8>(o, n, st);
+      return ops_launch(rmsnorm_kernel<T, 8, 512, Q8, false>, dim3(n.rows), dim3(512), 0, st, 1, n);
+  }
 }
 template <typename T>
 void rmsnorm_type(const asd_ops* o, const NormArgs& n, bool vec, bool q8, cudaStream_t st) {
-  if (vec)
-    q8 ? rmsnorm_t<T, 8, true>(o, n, st) : rmsnorm_t<T, 8, false>(o, n, st);
-  else
-    q8 ? rmsnorm_t<T, 1, true>(o, n, st) : rmsnorm_t<T, 1, false>(o, n, st);
+  q8 ? rmsnorm_t<T, true>(o, n, vec, st) : rmsnorm_t<T, false>(o, n, vec, st);
 }
 
-template <typename T, int VEC, int TPR>
-void quantize_rows(const asd_ops* o, QuantArgs n, cudaStream_t st) {
+template <typename T, int TPR>
+void quantize_rows(const asd_ops* o, QuantArgs n, bool vec, cudaStream_t st) {
   const int per_block = TPR == 32 ? 4 : 1;
-  constexpr int smem = quantize_smem<T, VEC, TPR>;
+  if (!vec) {
+    const WalkPlan p = plan_walk(o, n.rows, (int64_t)n.width * sizeof(T) * (n.act != ASD_ACT_NONE ? 2 : 1), 1, per_block, block_of<TPR>);
+    ops_launch(quantize_staged_kernel<T, TPR>, dim3(p.grid), dim3(block_of<TPR>), (size_t)p.smem, st, 1, n, p.k);
+    return;
+  }
+  constexpr int smem = quantize_smem<T, 8, TPR>;
   // as many blocks as the SMs hold together
   const int blocks = (n.rows + per_block - 1) / per_block, most = o->num_sms * (smem ? 232448 / (smem + 1024) : 1024 / block_of<TPR>);
   const int grid = blocks < most ? blocks : most;
   n.stride = grid * per_block;
-  ops_launch(quantize_kernel<T, VEC, TPR>, dim3(grid), dim3(block_of<TPR>), (size_t)smem, st, 1, n);
+  ops_launch(quantize_kernel<T, 8, TPR>, dim3(grid), dim3(block_of<TPR>), (size_t)smem, st, 1, n);
 }
-template <typename T, int VEC>
-void quantize_t(const asd_ops* o, const QuantArgs& n, cudaStream_t st) {
+template <typename T>
+void quantize_t(const asd_ops* o, const QuantArgs& n, bool vec, cudaStream_t st) {
   if (n.width > 512 * kPer) {
-    ops_launch(quantize_long_kernel<T, VEC>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    if (vec)
+      ops_launch(quantize_long_kernel<T, 8>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    else
+      ops_launch(quantize_long_kernel<T, 1>, dim3(n.rows), dim3(512), 0, st, 1, n);
     return;
   }
   switch (row_threads(o, n.rows, n.width)) {
-    case 32: return quantize_rows<T, VEC, 32>(o, n, st);
-    case 128: return quantize_rows<T, VEC, 128>(o, n, st);
-    case 256: return quantize_rows<T, VEC, 256>(o, n, st);
-    default: return quantize_rows<T, VEC, 512>(o, n, st);
+    case 32: return quantize_rows<T, 32>(o, n, vec, st);
+    case 128: return quantize_rows<T, 128>(o, n, vec, st);
+    case 256: return quantize_rows<T, 256>(o, n, vec, st);
+    default: return quantize_rows<T, 512>(o, n, vec, st);
   }
 }
 
@@ -807,14 +1025,18 @@ int grad_blocks(const asd_ops* o, int64_t rows, int width) {
   const int64_t most = (int64_t)per_sm * o->num_sms;
   return (int)(rows < most ? rows : most);
 }
+template <typename T, int VEC, int TPR>
+size_t grad_bytes(const NormGradArgs& n) {
+  return VEC == 8 ? (size_t)grad_smem<T, VEC, TPR, 16> : (size_t)(grad_ahead<T> + 1) * 3 * n.pitch;
+}
 template <typename T, int VEC>
 void grad_t(const asd_ops* o, const NormGradArgs& n, cudaStream_t st) {
   if (n.width <= 1024)
-    ops_launch(rmsnorm_grad_kernel<T, VEC, 64, 16>, dim3(n.blocks), dim3(64), (size_t)grad_smem<T, VEC, 64, 16>, st, 1, n);
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 64, 16>, dim3(n.blocks), dim3(64), grad_bytes<T, VEC, 64>(n), st, 1, n);
   else if (n.width <= 4096)
-    ops_launch(rmsnorm_grad_kernel<T, VEC, 256, 16>, dim3(n.blocks), dim3(256), (size_t)grad_smem<T, VEC, 256, 16>, st, 1, n);
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 256, 16>, dim3(n.blocks), dim3(256), grad_bytes<T, VEC, 256>(n), st, 1, n);
   else if (n.width <= kGradWidth)
-    ops_launch(rmsnorm_grad_kernel<T, VEC, 512, 16>, dim3(n.blocks), dim3(512), (size_t)grad_smem<T, VEC, 512, 16>, st, 1, n);
+    ops_launch(rmsnorm_grad_kernel<T, VEC, 512, 16>, dim3(n.blocks), dim3(512), grad_bytes<T, VEC, 512>(n), st, 1, n);
   else {
     ops_launch(rmsnorm_grad_long_kernel<T>, dim3(n.rows), dim3(512), 0, st, 1, n);
     if (n.part) ops_launch(columns_dw_kernel<T>, dim3((n.width + 127) / 128, n.blocks), dim3(128), 0, st, 1, n);
@@ -846,30 +1068,39 @@ void launch_quantize(const asd_ops* o, const asd_quantize_args* a, cudaStream_t 
   n.rows = a->rows, n.width = a->width, n.act = a->act, n.x = a->x, n.q = a->q, n.scale = a->scale, n.ld_x = a->ld_x, n.ld_q = a->ld_q;
   const bool vec = a->width % 8 == 0 && aligned(a->x, a->ld_x, ops_type_size(a->type), 16) && aligned(a->q, a->ld_q, 1, 8);
   if (a->type == ASD_TYPE_F32)
-    vec ? quantize_t<float, 8>(o, n, st) : quantize_t<float, 1>(o, n, st);
+    quantize_t<float>(o, n, vec, st);
   else if (a->type == ASD_TYPE_F16)
-    vec ? quantize_t<__half, 8>(o, n, st) : quantize_t<__half, 1>(o, n, st);
+    quantize_t<__half>(o, n, vec, st);
   else
-    vec ? quantize_t<__nv_bfloat16, 8>(o, n, st) : quantize_t<__nv_bfloat16, 1>(o, n, st);
+    quantize_t<__nv_bfloat16>(o, n, vec, st);
 }
 
 namespace {
-template <typename T>
-cudaError_t prepare_quantize() {
-  const cudaError_t e = cudaFuncSetAttribute(quantize_kernel<T, 8, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize, quantize_smem<T, 8, 256>);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(quantize_kernel<T, 8, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, quantize_smem<T, 8, 512>);
+template <typename K>
+cudaError_t allow_smem(K* kernel, int bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
-}  // namespace
-namespace {
+template <typename T, int TPR>
+cudaError_t prepare_staged() {
+  for (cudaError_t e : {allow_smem(rmsnorm_staged_kernel<T, TPR, true>, kStagedSmem), allow_smem(rmsnorm_staged_kernel<T, TPR, false>, kStagedSmem),
+                        allow_smem(quantize_staged_kernel<T, TPR>, kStagedSmem)})
+    if (e != cudaSuccess) return e;
+  return cudaSuccess;
+}
 template <typename T>
-cudaError_t prepare_grad() {
-  const cudaError_t e = cudaFuncSetAttribute(rmsnorm_grad_kernel<T, 8, 256, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, grad_smem<T, 8, 256, 16>);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(rmsnorm_grad_kernel<T, 8, 512, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, grad_smem<T, 8, 512, 16>);
+cudaError_t prepare_rows() {
+  for (cudaError_t e : {prepare_staged<T, 32>(), prepare_staged<T, 128>(), prepare_staged<T, 256>(), prepare_staged<T, 512>(),
+                        allow_smem(quantize_kernel<T, 8, 256>, quantize_smem<T, 8, 256>), allow_smem(quantize_kernel<T, 8, 512>, quantize_smem<T, 8, 512>),
+                        allow_smem(rmsnorm_grad_kernel<T, 8, 256, 16>, grad_smem<T, 8, 256, 16>),
+                        allow_smem(rmsnorm_grad_kernel<T, 8, 512, 16>, grad_smem<T, 8, 512, 16>),
+                        allow_smem(rmsnorm_grad_kernel<T, 1, 64, 16>, kStagedSmem), allow_smem(rmsnorm_grad_kernel<T, 1, 256, 16>, kStagedSmem),
+                        allow_smem(rmsnorm_grad_kernel<T, 1, 512, 16>, kStagedSmem)})
+    if (e != cudaSuccess) return e;
+  return cudaSuccess;
 }
 }  // namespace
 asd_status ops_rows_prepare() {
-  for (cudaError_t e : {prepare_quantize<__half>(), prepare_quantize<__nv_bfloat16>(), prepare_grad<float>(), prepare_grad<__half>(),
-                        prepare_grad<__nv_bfloat16>()})
+  for (cudaError_t e : {prepare_rows<float>(), prepare_rows<__half>(), prepare_rows<__nv_bfloat16>()})
     if (e != cudaSuccess) return ops_fail(ASD_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
   return ASD_OK;
 }
@@ -890,6 +1121,7 @@ void launch_rmsnorm_backward(const asd_ops* o, const asd_rmsnorm_backward_args* 
     n.rho = n.part + (size_t)n.blocks * a->width;
   }
   const int es = ops_type_size(a->type);
+  n.pitch = stage_pitch((int64_t)a->width * es);
   const bool vec = a->width % 8 == 0 && aligned(a->dy, a->ld_dy, es, 16) && aligned(a->s, a->ld_s, es, 16) &&
                    (!a->ds || aligned(a->ds, a->ld_ds, es, 16)) && (!a->weight || aligned(a->weight, 0, es, 16)) &&
                    (!a->dx || aligned(a->dx, a->ld_dx, es, 16));
