@@ -582,16 +582,22 @@ int64_t pair_kblocks(const OpsGemm& q) {
 // Clocks of a launch: the tiles go to the clusters in turn, and the longest row of them counts; some 10700 to start, drain
 // the last tile and end (measured at 64 tiles of 2 to 32 k-blocks).
 double list_clocks(const asd_ops* o, const OpsGemm* list, int count, int bn) {
-  const int units = o->num_sms / 2;
-  double load[256] = {};
-  int64_t first = 0;
+  const int units = std::min(o->num_sms / 2, 256);
+  double every = 0.0, more[256];  // of every cluster, and of some beyond that
+  std::fill(more, more + units, 0.0);
+  int next = 0;  // the cluster that the next product's first tile goes to
   for (int j = 0; j < count; ++j) {
-    const int64_t tiles = pair_tiles(list[j], bn), each = tiles / units;
+    const int64_t tiles = pair_tiles(list[j], bn);
+    const int rest = (int)(tiles % units);
     const double t = pair_kblocks(list[j]) * kblock_clocks(bn);
-    for (int u = 0; u < units; ++u) load[u] += t * (each + ((u - first % units + units) % units < tiles % units ? 1 : 0));
-    first += tiles;
+    every += t * (double)(tiles / units);
+    if (count == 1) return every + (rest ? t : 0.0) + 10700.0;
+    for (int i = 0; i < rest; ++i) {
+      more[next] += t;
+      if (++next == units) next = 0;
+    }
   }
-  return *std::max_element(load, load + units) + 10700.0;
+  return every + *std::max_element(more, more + units) + 10700.0;
 }
 template <int EPI>
 asd_status launch_width(const asd_ops* o, const OpsGemm* list, int count, cudaStream_t st) {

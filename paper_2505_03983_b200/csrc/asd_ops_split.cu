@@ -371,36 +371,41 @@ cudaError_t prepare_split() {
 // clocks a row; a launch 3000 and each wave of CTAs 4000; joining a cluster 2500 more, and one of eight, which the GPU finds
 // room for slowly, 9000 unless that is hidden under the kernel before (`early`).
 SplitPlan plan_split(const asd_ops* o, const OpsGemm& q, bool early) {
-  const int ke = q.epi == OPS_I8 ? 128 : 64, F = q.epi == OPS_GATE ? 64 : 128;
-  const int64_t kb = (q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0);
-  const int64_t tiles_n = (q.n + F - 1) / F;
-  const double weights = (double)tiles_n * kb * BM * 128;
-  SplitPlan best{16, 1, 2, 1e300};
-  const int64_t least = (q.m + 255) / 256;
-  for (int64_t blocks = least; blocks <= 4 * least + 16; ++blocks) {
-    const int nb = (int)std::max<int64_t>(16, ((q.m + blocks - 1) / blocks + 15) / 16 * 16);
-    if (nb > 256) continue;
-    const int64_t tiles_m = (q.m + nb - 1) / nb;
+  const int ke = q.epi == OPS_I8 ? 128 : 64, F = q.epi == OPS_GATE ? 64 : 128, m = (int)q.m, sms = o->num_sms;
+  const int kb = (int)((q.k[0] + ke - 1) / ke + (q.parts == 2 ? (q.k[1] + ke - 1) / ke : 0));
+  const int tiles_n = (int)((q.n + F - 1) / F);
+  const float weights = (float)tiles_n * kb * (BM * 128);
+  SplitPlan best{16, 1, 2, 1e30};
+  int side_of_best = 1, share_of_best = kb;
+  int last = 0;  // CTAs along the rows of the candidate before: of several heights with the same number the least one counts
+  for (int nb = 16; nb <= 256; nb += 16) {
+    const int tiles_m = (m + nb - 1) / nb;
+    if (tiles_m == last) continue;
+    last = tiles_m;
     for (int split = 1; split <= 8; split *= 2) {
-      if (split > 1 && kb / split < 2) break;
-      const int64_t ctas = tiles_n * tiles_m * split, share = (kb + split - 1) / split;
+      if (split > 1 && kb < 2 * split) break;
+      const int64_t all = (int64_t)tiles_n * tiles_m * split;
+      if (all > 1 << 20) break;
+      const int ctas = (int)all, share = (kb + split - 1) / split;
       // CTAs that run side by side on an SM
-      int side = (int)std::min<int64_t>(3, (ctas + o->num_sms - 1) / o->num_sms);
+      int side = std::min(3, (ctas + sms - 1) / sms);
       while (side > 1 && side * (split_smem(nb, 2) + 1024) > kSmSmem) --side;
-      const int64_t waves = (ctas + side * o->num_sms - 1) / (side * o->num_sms);
-      const double fill = side * (BM + nb) * 128 / 64.0, math = side * std::max(128.0, 2.0 * nb);
-      const double stream = weights / (23.0 * std::min<int64_t>(ctas, o->num_sms)) / waves;
-      const double join = split == 8 && !early ? 9000.0 : split > 1 ? 2500.0 : 0.0;
-      const double t = 3000.0 + waves * (4000.0 + join + std::max(stream, share * std::max(fill, math)) + 37.0 * nb / split);
-      if (t < best.clocks) {
-        // few rows: no more than half of the SM's shared memory, which leaves room for the next kernel's first weights
-        int stages = (int)std::min<int64_t>(nb <= 64 ? 112 * 1024 / split_stage_bytes(nb) : kMostStages, std::max<int64_t>(2, share));
-        while (stages > 2 && side * (split_smem(nb, stages) + 1024) > kSmSmem) --stages;
-        best = SplitPlan{nb, split, stages, t};
+      const int waves = (ctas + side * sms - 1) / (side * sms);
+      const float fill = side * (BM + nb) * 2.f, math = side * std::max(128.f, 2.f * nb);
+      const float stream = weights / (23.f * std::min(ctas, sms)) / waves;
+      const float join = split == 8 && !early ? 9000.f : split > 1 ? 2500.f : 0.f;
+      const float c = 3000.f + waves * (4000.f + join + std::max(stream, share * std::max(fill, math)) + 37.f * nb / split);
+      if (c < best.clocks) {
+        best = SplitPlan{nb, split, 2, c};
+        side_of_best = side;
+        share_of_best = share;
       }
     }
-    if (nb == 16) break;
   }
+  // few rows: no more than half of the SM's shared memory, which leaves room for the next kernel's first weights
+  best.stages = std::min(best.nb <= 64 ? 112 * 1024 / split_stage_bytes(best.nb) : kMostStages, std::max(2, share_of_best));
+  best.stages = std::min(best.stages, kMostStages);
+  while (best.stages > 2 && side_of_best * (split_smem(best.nb, best.stages) + 1024) > kSmSmem) --best.stages;
   return best;
 }
 
