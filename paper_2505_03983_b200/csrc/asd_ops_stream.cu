@@ -19,7 +19,7 @@ constexpr int kStreamWarps = 16;
 
 constexpr int kStreamSmem = 232448;
 // Shared memory of x and the partial sums.
-int64_t rows_bytes(int64_t rows, int64_t pitch) { return rows * (pitch + 2 * kStreamWarps * 17 * 4); }
+int64_t rows_bytes(int64_t rows, int64_t pitch) { return rows * pitch + 2 * kStreamWarps * ((rows * 17) | 1) * 4; }
 constexpr int ring_bytes(int ring) { return kStreamWarps * ring * 1024; }
 
 struct StreamArgs {
@@ -42,13 +42,6 @@ struct StreamArgs {
 __device__ __forceinline__ void copy_16(uint32_t dst, const uint8_t* src, int bytes) {
   asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-// The last bytes of a row: what lies beyond it counts as zero.
-__device__ __forceinline__ uint4 load_part(const uint8_t* p, int bytes) {
-  uint32_t w[4] = {0, 0, 0, 0};
-  for (int i = 0; i < min(bytes, 16); ++i) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 enum { KIND_F16 = 0, KIND_BF16 = 1, KIND_I8 = 2 };
 // acc += w x^T for 32 bytes of k (words a of rows g and g + 8, words b of row g of x).
 template <int KIND>
@@ -89,8 +82,9 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
   uint8_t* ring = smem + warp * (RING * 1024) + lane * 16;
   const uint32_t ring_addr = smem_u32(ring);
   uint8_t* xs = smem + kStreamWarps * RING * 1024;
-  // a warp's sums, [2][warp][row of x][16 rows of w and one word that keeps rows on different banks]
+  // the warps' sums, [2][warp][row of x][16 rows of w]
   uint32_t* part = reinterpret_cast<uint32_t*>(xs + a.rows * a.pitch);
+  const uint32_t xs_addr = smem_u32(xs);
 
   // The copies run ahead of the sums through the same sequence: steps s0 .. s1 of the block's first rows, then of its next.
   int unit = s0 < s1 ? 0 : mine, step = s0, slot = 0;
@@ -114,23 +108,35 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (!a.early) grid_dependency_wait();
+  // x: each warp brings its own share of k, so that no barrier of the block is needed; ahead of the weights, behind which it
+  // would wait for as long as a whole ring of them takes
+  auto copy_x = [&]() {
+    for (int r = 0; r < a.rows; ++r) {
+      for (int s = s0 * 4 + lane; s < s1 * 4; s += 32) {
+        const int left = min(max(a.k_bytes - s * 16, 0), 16);
+        copy_16(xs_addr + r * a.pitch + s * 16, a.x + r * a.ld_x + (left ? (int64_t)s * 16 : 0), left);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
   if (unit < mine) rows_of(0);
+  if (!a.early) {
+    grid_dependency_wait();
+    copy_x();
+  }
 #pragma unroll
   for (int i = 0; i < RING - 1; ++i) copy_next();
-  if (a.early) grid_dependency_wait();
-  grid_launch_dependents();
-
-  // x: each warp brings its own share of k, so that no barrier is needed
-  for (int r = 0; r < a.rows; ++r) {
-    for (int s = s0 * 4 + lane; s < s1 * 4; s += 32) {
-      const uint8_t* p = a.x + r * a.ld_x + (int64_t)s * 16;
-      const int left = a.k_bytes - s * 16;
-      *reinterpret_cast<uint4*>(xs + r * a.pitch + s * 16) = left >= 16 ? *reinterpret_cast<const uint4*>(p) : load_part(p, left);
-    }
+  if (a.early) {
+    grid_dependency_wait();
+    copy_x();
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+  } else {
+    asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");  // all but the ring's
   }
+  grid_launch_dependents();
   __syncwarp();
 
+  const int of_row = 17, of_warp = (a.rows * 17) | 1;  // words from a row's, a warp's sums to the next: odd, for the banks
   const uint8_t* xr = xs + g * a.pitch + 16 * t;
   const bool have = g < a.rows;
   int at = 0;
@@ -147,7 +153,6 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
       if (++at == RING) at = 0;
     }
     // free: every thread has passed the barrier of unit i - 1 after reading unit i - 2's
-    const int of_row = 17, of_warp = a.rows * 17;
     uint32_t* p = part + (i & 1) * kStreamWarps * of_warp;
     uint32_t* own = p + warp * of_warp + g;
     if (2 * t < a.rows) {
@@ -158,37 +163,62 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
       own[(2 * t + 1) * of_row] = acc[1];
       own[(2 * t + 1) * of_row + 8] = acc[3];
     }
+    // 16 lanes add up the warps' sums of one output, two outputs to a warp at a time: every warp has the same share.  The
+    // scales come before the barrier.
+    constexpr int TURNS = FR * 8 / (2 * kStreamWarps);
+    const int col0 = ((int)blockIdx.x + i * (int)gridDim.x) * FR, from = lane & 15;
+    float scale[TURNS][3];
+#pragma unroll
+    for (int j = 0; j < TURNS; ++j) {
+      const int o = 2 * (warp + j * kStreamWarps) + (lane >> 4), col = col0 + o % FR;
+      scale[j][0] = scale[j][1] = scale[j][2] = 0.f;
+      if (KIND == KIND_I8 && o < FR * a.rows && col < a.n && from == 0) {
+        scale[j][0] = a.scale_a[o / FR];
+        scale[j][1] = a.scale_b[col];
+        if (a.bias) scale[j][2] = a.bias[col];
+      }
+    }
     __syncthreads();
-    const int f = threadIdx.x % FR, row = threadIdx.x / FR, col = ((int)blockIdx.x + i * (int)gridDim.x) * FR + f;
-    if (row >= a.rows || col >= a.n) continue;
-    const uint32_t* sums = p + row * of_row + f;
-    if constexpr (KIND == KIND_I8) {
-      int v = 0;
 #pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) v += (int)sums[w * of_warp];
-      const float y = fmaf((float)v * a.scale_a[row], a.scale_b[col], a.bias ? a.bias[col] : 0.f);
-      if (a.out_type == ASD_TYPE_F32)
-        reinterpret_cast<float*>(a.c)[row * a.ldc + col] = y;
-      else
-        reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(y, a.out_type == ASD_TYPE_F16);
-    } else {
-      float v = 0.f, u = 0.f;
+    for (int j = 0; j < TURNS; ++j) {
+      if (2 * (warp + j * kStreamWarps) >= FR * a.rows) break;
+      const int o = 2 * (warp + j * kStreamWarps) + (lane >> 4);
+      const bool any = o < FR * a.rows;
+      const int f = o % FR, row = any ? o / FR : 0, col = col0 + f;
+      const bool out = any && col < a.n && from == 0;
+      const uint32_t* sum = p + from * of_warp + row * of_row + f;
+      if constexpr (KIND == KIND_I8) {
+        int v = (int)sum[0];
 #pragma unroll
-      for (int w = 0; w < kStreamWarps; ++w) {
-        v += __uint_as_float(sums[w * of_warp]);
-        if (EPI == OPS_GATE) u += __uint_as_float(sums[w * of_warp + 8]);
-      }
-      if (EPI == OPS_GATE) {
-        float g1[1] = {v}, u1[1] = {u}, h1[1];
-        gated(g1, u1, h1, a.gelu != 0, a.kept != nullptr);
-        if (a.kept) {
-          uint8_t* b = a.kept + kept_offset(row, col, a.kept_cols);
-          kept_put(b, row, col & 31, g1[0]);
-          kept_put(b + kKeptHalf, row, col & 31, u1[0]);
+        for (int d = 8; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        const float y = fmaf((float)v * scale[j][0], scale[j][1], scale[j][2]);
+        if (out) {
+          if (a.out_type == ASD_TYPE_F32)
+            reinterpret_cast<float*>(a.c)[row * a.ldc + col] = y;
+          else
+            reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(y, a.out_type == ASD_TYPE_F16);
         }
-        v = h1[0];
+      } else {
+        float v = __uint_as_float(sum[0]), u = EPI == OPS_GATE ? __uint_as_float(sum[8]) : 0.f;
+#pragma unroll
+        for (int d = 8; d; d >>= 1) {
+          v += __shfl_xor_sync(0xffffffffu, v, d);
+          if (EPI == OPS_GATE) u += __shfl_xor_sync(0xffffffffu, u, d);
+        }
+        if (out) {
+          if (EPI == OPS_GATE) {
+            float g1[1] = {v}, u1[1] = {u}, h1[1];
+            gated(g1, u1, h1, a.gelu != 0, a.kept != nullptr);
+            if (a.kept) {
+              uint8_t* b = a.kept + kept_offset(row, col, a.kept_cols);
+              kept_put(b, row, col & 31, g1[0]);
+              kept_put(b + kKeptHalf, row, col & 31, u1[0]);
+            }
+            v = h1[0];
+          }
+          reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(v, KIND == KIND_F16);
+        }
       }
-      reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(v, KIND == KIND_F16);
     }
   }
 }
