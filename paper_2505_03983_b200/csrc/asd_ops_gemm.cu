@@ -15,6 +15,11 @@
 //              the other the value's): h = act(g) u, and its two derivatives kept for the backward pass
 //   GATE_GRAD  C = dh: dg = dh u act'(g), du = dh act(g), from the two factors that were kept
 //   I8         C scale_a[m] scale_b[n] + bias[n], rounded to the output's type
+// Measured at 8192 x 2048 x 8192 in bf16, one launch at 1.6 GHz: gate 391 to 420 us with what is kept (1.3 PFLOP/s), h Wo 205 to 223
+// (1.2 to 1.3), gate gradient 213 to 228, the three gradient products 1.0 ms (1.3 to 1.35); int8 8192 x 4096 x 8192 216 to 225 us
+// (2.5 POP/s).  A k-block of a 256 x 256 tile takes some 650 clocks: its MMAs 512, but its 80 KB of shared memory traffic 640.  In
+// a loop the power limit bounds all of them (988 W at 1.4 to 1.5 GHz).  Twice as high tiles (512 x 256) need fewer bytes and take
+// longer (383 against 335 thousand clocks).
 // An output whose address and row distance are multiples of 16 bytes leaves through shared memory by TMA stores of 128-byte
 // row pieces; the others are staged in the same way and stored by lanes on neighbouring elements.
 #include <limits.h>

@@ -10,6 +10,9 @@
 // bf16 took 127 us to quantise).
 #include <type_traits>
 
+//
+// Measured (of 6.55 TB/s): norm 8192 x 4096 bf16 43 us = 6.2 TB/s, to int8 32768 x 1024 42.6 us = 5.5 TB/s, gradient 8192 x 4096 52 us =
+// 5.2 TB/s, gate to int8 8192 x 8192 56.6 us = 5.9 TB/s.  One row of 4096 takes 4 us, a kernel's start and end.
 #include "asd_ops_act.cuh"
 #include "asd_ops_internal.h"
 

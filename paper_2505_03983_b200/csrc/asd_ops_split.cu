@@ -6,6 +6,10 @@
 // store 32 neighbouring columns of a row of C.  Each CTA parks its partial sums in its own shared memory as
 // [row of C][column]; after one cluster barrier every CTA adds up its share of the rows over distributed shared memory in
 // the order of the ranks (the same bits in every run), applies the epilogue and stores.
+//
+// Measured: the gated MLP of 16 rows, 4096 x 8192 in 16 bits, 201 MB of weights in 40 us (5.0 TB/s) against 80 with tiles; int8
+// 64 x 4096 x 4096 7.9 us against 14.7, 256 x 4096 x 4096 11.3 against 15.5; at 512 x 1024 x 4096 both take 8 and the tiles go on
+// from there.  What bounds it beside the weights is a kernel's start, the join and the way of the operands into shared memory.
 #include <string.h>
 
 #include <algorithm>

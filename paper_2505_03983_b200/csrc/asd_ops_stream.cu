@@ -8,6 +8,11 @@
 // weights come through a ring in shared memory of its own (cp.async, up to 11 steps of 1 KB a warp ahead, 176 KB an SM),
 // which needs neither barriers nor registers, and runs on over the block's next rows while the sums of one group of rows
 // meet (in shared memory, in a fixed order).
+//
+// Measured: 155 MB of int8 weights (1 x 8192 x 18944) in 25.1 us = 6.2 TB/s; 34 MB (1 x 4096 x 8192) in 8.3 us, of which 5.3 are
+// the bytes and the rest a kernel's start, first and last byte.  The split kernel, whose weights are the 128-row operand of
+// tcgen05, has tensor memory to allocate and cluster barriers to pass: gated MLP 1 x 1024 x 4096 12.4 us against 7.7 here, int8
+// 1 x 1024 x 1024 3.5 against 2.0.  At 8 rows they meet (int8 8 x 4096 x 8192: 9.3 and 9.7; gated MLP 8 x 4096 x 8192: 37.8 and 37.2).
 #include <algorithm>
 
 #include "asd_ops_tc.cuh"
@@ -67,8 +72,8 @@ __device__ __forceinline__ void mma_16x8(uint32_t (&c)[4], uint32_t a0, uint32_t
   }
 }
 
-// RING: steps of the ring.
-template <int KIND, int EPI, int RING>
+// RING: steps of the ring.  SPAN: lanes that add up the warps' sums of one output.
+template <int KIND, int EPI, int RING, int SPAN>
 __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const StreamArgs a) {
   constexpr int FR = EPI == OPS_GATE ? 8 : 16;  // columns of the output to a group of rows of w
   extern __shared__ __align__(128) uint8_t smem[];  // the warps' rings, x, the warps' sums
@@ -111,12 +116,15 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
   // x: each warp brings its own share of k, so that no barrier of the block is needed; ahead of the weights, behind which it
   // would wait for as long as a whole ring of them takes
   auto copy_x = [&]() {
-    for (int r = 0; r < a.rows; ++r) {
-      for (int s = s0 * 4 + lane; s < s1 * 4; s += 32) {
+    const int pieces = (s1 - s0) * 4, all = a.rows * pieces;  // of 16 bytes, of a row and of all; lanes take them in turn
+    for (int at = 0; at < all; at += 32) {
+      const int r = (at + lane) / pieces, s = s0 * 4 + at + lane - r * pieces;
+      if (r < a.rows) {
         const int left = min(max(a.k_bytes - s * 16, 0), 16);
         copy_16(xs_addr + r * a.pitch + s * 16, a.x + r * a.ld_x + (left ? (int64_t)s * 16 : 0), left);
       }
     }
+    __syncwarp();
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   if (unit < mine) rows_of(0);
@@ -137,6 +145,59 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
   __syncwarp();
 
   const int of_row = 17, of_warp = (a.rows * 17) | 1;  // words from a row's, a warp's sums to the next: odd, for the banks
+  // One output: its sum v (GATE: of g, and u) is complete.
+  auto finish = [&](int row, int col, uint32_t v, uint32_t u, float sa, float sb, float bb) {
+    if constexpr (KIND == KIND_I8) {
+      const float y = fmaf((float)(int)v * sa, sb, bb);
+      if (a.out_type == ASD_TYPE_F32)
+        reinterpret_cast<float*>(a.c)[row * a.ldc + col] = y;
+      else
+        reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(y, a.out_type == ASD_TYPE_F16);
+    } else {
+      float h[1] = {__uint_as_float(v)};
+      if (EPI == OPS_GATE) {
+        float g1[1] = {h[0]}, u1[1] = {__uint_as_float(u)};
+        gated(g1, u1, h, a.gelu != 0, a.kept != nullptr);
+        if (a.kept) {
+          uint8_t* b = a.kept + kept_offset(row, col, a.kept_cols);
+          kept_put(b, row, col & 31, g1[0]);
+          kept_put(b + kKeptHalf, row, col & 31, u1[0]);
+        }
+      }
+      reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(h[0], KIND == KIND_F16);
+    }
+  };
+  auto add = [&](uint32_t x, uint32_t y) { return KIND == KIND_I8 ? x + y : __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); };
+  // The warps' sums of unit i meet: SPAN lanes to an output, 32 / SPAN outputs to a warp, in an order that depends on nothing
+  // else.  16 lanes each where there are few outputs, four where 16 would have to take turns (9.8 against 12.5 us, gated MLP
+  // 8 x 1024 x 4096).  Scales are fetched before the barrier.
+  auto join = [&](int i, const uint32_t* p) {
+    constexpr int OUTS = 32 / SPAN;
+    const int o = OUTS * warp + lane / SPAN, f = o % FR, row = o / FR, from = lane % SPAN;
+    const int col = ((int)blockIdx.x + i * (int)gridDim.x) * FR + f;
+    const bool out = row < a.rows && col < a.n && from == 0;
+    float sa = 0.f, sb = 0.f, bb = 0.f;
+    if (KIND == KIND_I8 && out) {
+      sa = a.scale_a[row];
+      sb = a.scale_b[col];
+      if (a.bias) bb = a.bias[col];
+    }
+    __syncthreads();
+    if (OUTS * warp >= FR * a.rows) return;
+    const uint32_t* sum = p + from * of_warp + (row < a.rows ? row : 0) * of_row + f;
+    uint32_t v = sum[0], u = EPI == OPS_GATE ? sum[8] : 0u;
+#pragma unroll
+    for (int k = 1; k < kStreamWarps / SPAN; ++k) {
+      v = add(v, sum[k * SPAN * of_warp]);
+      if (EPI == OPS_GATE) u = add(u, sum[k * SPAN * of_warp + 8]);
+    }
+#pragma unroll
+    for (int d = SPAN / 2; d; d >>= 1) {
+      v = add(v, __shfl_xor_sync(0xffffffffu, v, d));
+      if (EPI == OPS_GATE) u = add(u, __shfl_xor_sync(0xffffffffu, u, d));
+    }
+    if (out) finish(row, col, v, u, sa, sb, bb);
+  };
   const uint8_t* xr = xs + g * a.pitch + 16 * t;
   const bool have = g < a.rows;
   int at = 0;
@@ -163,87 +224,45 @@ __global__ void __launch_bounds__(32 * kStreamWarps, 1) stream_kernel(const Stre
       own[(2 * t + 1) * of_row] = acc[1];
       own[(2 * t + 1) * of_row + 8] = acc[3];
     }
-    // 16 lanes add up the warps' sums of one output, two outputs to a warp at a time: every warp has the same share.  The
-    // scales come before the barrier.
-    constexpr int TURNS = FR * 8 / (2 * kStreamWarps);
-    const int col0 = ((int)blockIdx.x + i * (int)gridDim.x) * FR, from = lane & 15;
-    float scale[TURNS][3];
-#pragma unroll
-    for (int j = 0; j < TURNS; ++j) {
-      const int o = 2 * (warp + j * kStreamWarps) + (lane >> 4), col = col0 + o % FR;
-      scale[j][0] = scale[j][1] = scale[j][2] = 0.f;
-      if (KIND == KIND_I8 && o < FR * a.rows && col < a.n && from == 0) {
-        scale[j][0] = a.scale_a[o / FR];
-        scale[j][1] = a.scale_b[col];
-        if (a.bias) scale[j][2] = a.bias[col];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < TURNS; ++j) {
-      if (2 * (warp + j * kStreamWarps) >= FR * a.rows) break;
-      const int o = 2 * (warp + j * kStreamWarps) + (lane >> 4);
-      const bool any = o < FR * a.rows;
-      const int f = o % FR, row = any ? o / FR : 0, col = col0 + f;
-      const bool out = any && col < a.n && from == 0;
-      const uint32_t* sum = p + from * of_warp + row * of_row + f;
-      if constexpr (KIND == KIND_I8) {
-        int v = (int)sum[0];
-#pragma unroll
-        for (int d = 8; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-        const float y = fmaf((float)v * scale[j][0], scale[j][1], scale[j][2]);
-        if (out) {
-          if (a.out_type == ASD_TYPE_F32)
-            reinterpret_cast<float*>(a.c)[row * a.ldc + col] = y;
-          else
-            reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(y, a.out_type == ASD_TYPE_F16);
-        }
-      } else {
-        float v = __uint_as_float(sum[0]), u = EPI == OPS_GATE ? __uint_as_float(sum[8]) : 0.f;
-#pragma unroll
-        for (int d = 8; d; d >>= 1) {
-          v += __shfl_xor_sync(0xffffffffu, v, d);
-          if (EPI == OPS_GATE) u += __shfl_xor_sync(0xffffffffu, u, d);
-        }
-        if (out) {
-          if (EPI == OPS_GATE) {
-            float g1[1] = {v}, u1[1] = {u}, h1[1];
-            gated(g1, u1, h1, a.gelu != 0, a.kept != nullptr);
-            if (a.kept) {
-              uint8_t* b = a.kept + kept_offset(row, col, a.kept_cols);
-              kept_put(b, row, col & 31, g1[0]);
-              kept_put(b + kKeptHalf, row, col & 31, u1[0]);
-            }
-            v = h1[0];
-          }
-          reinterpret_cast<uint16_t*>(a.c)[row * a.ldc + col] = round16(v, KIND == KIND_F16);
-        }
-      }
-    }
+    join(i, p);
   }
 }
 
-template <int KIND, int EPI>
-void launch_stream(const asd_ops* o, const StreamArgs& a, cudaStream_t st) {
+template <int KIND, int EPI, int SPAN>
+void launch_span(const asd_ops* o, const StreamArgs& a, cudaStream_t st) {
   const int fr = EPI == OPS_GATE ? 8 : 16;
   const dim3 grid(std::min((a.n + fr - 1) / fr, o->num_sms)), block(32 * kStreamWarps);
   const int x = (int)rows_bytes(a.rows, a.pitch);
-  // The ring: no longer than a warp has steps, so that the next kernel's blocks find room beside these; of a kernel that
-  // may start early the shortest, for it has to fit beside the one before.
+  // The ring: no longer than a warp has steps, so that the next kernel's blocks may find room beside these.  (The shortest for a
+  // kernel that may start early, so that it always does, is slower: 9.0 against 7.6 us, gated MLP 1 x 1024 x 4096.)
   const int units = (a.n + fr - 1) / fr, steps = (a.k_bytes + 63) / 64;
   const int most = (units + (int)grid.x - 1) / (int)grid.x * ((steps + kStreamWarps - 1) / kStreamWarps);
-  if (x <= kStreamSmem - ring_bytes(12) && most > 8 && !a.early)
-    ops_launch(stream_kernel<KIND, EPI, 12>, grid, block, (size_t)(ring_bytes(12) + x), st, 1, a);
-  else if (x <= kStreamSmem - ring_bytes(8) && most > 4 && !a.early)
-    ops_launch(stream_kernel<KIND, EPI, 8>, grid, block, (size_t)(ring_bytes(8) + x), st, 1, a);
+  if (x <= kStreamSmem - ring_bytes(12) && most > 8)
+    ops_launch(stream_kernel<KIND, EPI, 12, SPAN>, grid, block, (size_t)(ring_bytes(12) + x), st, 1, a);
+  else if (x <= kStreamSmem - ring_bytes(8) && most > 4)
+    ops_launch(stream_kernel<KIND, EPI, 8, SPAN>, grid, block, (size_t)(ring_bytes(8) + x), st, 1, a);
   else
-    ops_launch(stream_kernel<KIND, EPI, 4>, grid, block, (size_t)(ring_bytes(4) + x), st, 1, a);
+    ops_launch(stream_kernel<KIND, EPI, 4, SPAN>, grid, block, (size_t)(ring_bytes(4) + x), st, 1, a);
+}
+template <int KIND, int EPI>
+void launch_stream(const asd_ops* o, const StreamArgs& a, cudaStream_t st) {
+  if ((EPI == OPS_GATE ? 8 : 16) * a.rows <= 2 * kStreamWarps)
+    launch_span<KIND, EPI, 16>(o, a, st);
+  else
+    launch_span<KIND, EPI, 4>(o, a, st);
 }
 template <int KIND, int EPI>
 cudaError_t prepare_stream() {
-  cudaError_t e = cudaFuncSetAttribute(stream_kernel<KIND, EPI, 12>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(stream_kernel<KIND, EPI, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(stream_kernel<KIND, EPI, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+  cudaError_t e = cudaSuccess;
+  auto set = [&](auto* kernel) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+  };
+  set(stream_kernel<KIND, EPI, 12, 16>);
+  set(stream_kernel<KIND, EPI, 8, 16>);
+  set(stream_kernel<KIND, EPI, 4, 16>);
+  set(stream_kernel<KIND, EPI, 12, 4>);
+  set(stream_kernel<KIND, EPI, 8, 4>);
+  set(stream_kernel<KIND, EPI, 4, 4>);
   return e;
 }
 
