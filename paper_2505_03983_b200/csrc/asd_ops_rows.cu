@@ -8,11 +8,11 @@
 // multiple of 8 elements come into shared memory in the aligned 16-byte pieces that hold them, one row ahead, and are read
 // from there element by element, neighbouring threads on neighbouring elements (read so from memory, 6001 rows of 2 x 2477
 // bf16 took 127 us to quantise).
-#include <type_traits>
-
 //
 // Measured (of 6.55 TB/s): norm 8192 x 4096 bf16 43 us = 6.2 TB/s, to int8 32768 x 1024 42.6 us = 5.5 TB/s, gradient 8192 x 4096 52 us =
 // 5.2 TB/s, gate to int8 8192 x 8192 56.6 us = 5.9 TB/s.  One row of 4096 takes 4 us, a kernel's start and end.
+#include <type_traits>
+
 #include "asd_ops_act.cuh"
 #include "asd_ops_internal.h"
 
@@ -219,13 +219,19 @@ __device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
 }
 
 // A row of `bytes` into shared memory by T threads, in aligned pieces; it starts (address & 15) bytes into dst.  Nothing
-// beyond the row's end is read; before its start, the rest of the piece that holds it.
-__device__ __forceinline__ void stage_row(uint8_t* dst, const void* src, int bytes, int t, int T) {
-  const uint8_t* p = reinterpret_cast<const uint8_t*>((uintptr_t)src & ~(uintptr_t)15);
-  const int end = bytes + (int)((uintptr_t)src & 15);
-  for (int at = 16 * t; at < end; at += 16 * T)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + at)), "l"(p + at), "r"(min(16, end - at))
-                 : "memory");
+// beyond the row's end is read.  The piece that holds its start begins in the row before; where there is none (`top`) one
+// thread copies what there is of it.
+__device__ __forceinline__ void stage_row(uint8_t* dst, const void* src, int bytes, int t, int T, bool top) {
+  const int off = (int)((uintptr_t)src & 15), end = bytes + off;
+  const uint8_t* p = reinterpret_cast<const uint8_t*>(src) - off;
+  for (int at = 16 * t; at < end; at += 16 * T) {
+    if (at == 0 && top && off) {
+      for (int i = off; i < min(16, end); i += 2) *reinterpret_cast<uint16_t*>(dst + i) = *reinterpret_cast<const uint16_t*>(p + i);
+    } else {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + at)), "l"(p + at), "r"(min(16, end - at))
+                   : "memory");
+    }
+  }
 }
 template <typename T>
 __device__ __forceinline__ const T* staged(const uint8_t* dst, const void* src) {
@@ -293,8 +299,8 @@ __global__ void __launch_bounds__(block_of<TPR>) rmsnorm_staged_kernel(const Nor
   walk_rows<TPR>(
       TPR == 32 ? blockIdx.x * 4 + slot : blockIdx.x, a.rows, k,
       [&](int row, int turn) {
-        stage_row(buffer(turn, 0), xrow(row), a.width * (int)sizeof(T), t, TPR);
-        if (a.r) stage_row(buffer(turn, 1), rrow(row), a.width * (int)sizeof(T), t, TPR);
+        stage_row(buffer(turn, 0), xrow(row), a.width * (int)sizeof(T), t, TPR, row == 0);
+        if (a.r) stage_row(buffer(turn, 1), rrow(row), a.width * (int)sizeof(T), t, TPR, row == 0);
       },
       [&](int row, int turn) {
         const T* x = staged<T>(buffer(turn, 0), xrow(row)) + t;
@@ -579,7 +585,7 @@ __global__ void __launch_bounds__(block_of<TPR>) quantize_staged_kernel(const Qu
   int side = 0;
   walk_rows<TPR>(
       TPR == 32 ? blockIdx.x * 4 + slot : blockIdx.x, a.rows, k,
-      [&](int row, int turn) { stage_row(mine + turn * k.pitch, xrow(row), (gate ? 2 : 1) * a.width * (int)sizeof(T), t, TPR); },
+      [&](int row, int turn) { stage_row(mine + turn * k.pitch, xrow(row), (gate ? 2 : 1) * a.width * (int)sizeof(T), t, TPR, row == 0); },
       [&](int row, int turn) {
         const T* x = staged<T>(mine + turn * k.pitch, xrow(row)) + t;
         float f[kPer];
@@ -702,7 +708,7 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
   auto fetch = [&](int64_t row, int turn) {
     if (!AHEAD && row < a.rows) {
       for (int part = 0; part < 3; ++part)
-        if (part < 2 || a.ds) stage_row(staged_at(turn, part), base[part] + row * ld[part], a.width * (int)sizeof(T), t, TPR);
+        if (part < 2 || a.ds) stage_row(staged_at(turn, part), base[part] + row * ld[part], a.width * (int)sizeof(T), t, TPR, row == 0);
     }
     if (AHEAD && row < a.rows) {
 #pragma unroll
