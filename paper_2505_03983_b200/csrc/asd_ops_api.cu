@@ -161,6 +161,11 @@ asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, 
   if (a->dx) w = aligned_operand(Mat{a->w_in, 2 * (int64_t)a->hidden, a->width, a->ld_w_in, 2}, cut, &packs);
   if (inner) wo = aligned_operand(Mat{a->w_out, a->width, a->hidden, a->ld_w_out, 2}, cut, &packs);
   uint8_t* dgu = inner ? (uint8_t*)cut->take(rows * 2 * hp * 2) : nullptr;  // [rows, dg | du], each padded
+  // the weights' gradients are sums over all rows: few outputs in slices
+  const int s_in = a->dw_in ? sum_slices(o, a->hidden, a->width, rows) : 1, s_out = a->dw_out ? sum_slices(o, a->width, a->hidden, rows) : 1;
+  float* part_in[2];
+  for (float*& p : part_in) p = (float*)cut->take(part_bytes(a->hidden, a->width, s_in));
+  float* part_out = (float*)cut->take(part_bytes(a->width, a->hidden, s_out));
   if (!launch) return ASD_OK;
   launch_packs(o, packs, st);
   const Mat dg{dgu, rows, a->hidden, 2 * hp, 2}, du{dgu + 2 * hp, rows, a->hidden, 2 * hp, 2};
@@ -188,11 +193,15 @@ asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, 
     g.b[1] = {Mat{(const uint8_t*)w.p + 2 * w.ld * a->hidden, a->hidden, w.cols, w.ld, 2}, true};
   }
   if (a->dw_in) {  // dg^T x, du^T x
-    product({dg, true}, {x, true}, a->dw_in, a->ld_dw_in, a->hidden, a->width, rows);
-    product({du, true}, {x, true}, (uint8_t*)a->dw_in + 2 * a->ld_dw_in * a->hidden, a->ld_dw_in, a->hidden, a->width, rows);
+    for (int i = 0; i < 2; ++i) {
+      OpsGemm& g = product({i ? du : dg, true}, {x, true}, (uint8_t*)a->dw_in + i * 2 * a->ld_dw_in * a->hidden, a->ld_dw_in, a->hidden, a->width, rows);
+      g.slices = s_in, g.part = part_in[i];
+    }
   }
-  if (a->dw_out)  // dy^T h
-    product({dy, true}, {Mat{a->saved, rows, a->hidden, hp, 2}, true}, a->dw_out, a->ld_dw_out, a->width, a->hidden, rows);
+  if (a->dw_out) {  // dy^T h
+    OpsGemm& g = product({dy, true}, {Mat{a->saved, rows, a->hidden, hp, 2}, true}, a->dw_out, a->ld_dw_out, a->width, a->hidden, rows);
+    g.slices = s_out, g.part = part_out;
+  }
   return ops_gemm_list(o, list, n, st);
 }
 

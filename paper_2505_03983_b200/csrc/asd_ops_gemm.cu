@@ -40,13 +40,16 @@ namespace {
 
 constexpr int kStoreBytes = 32 * 128;  // a warp's staging buffer: 32 rows of 128 bytes
 constexpr int kBand = 8;               // tile rows that are walked over together
+constexpr int kPartBlock = 32 * 32;    // partial sums of a block
 
 // One product of a launch.
 struct PairProduct {
   int m, n;       // of C (GATE: n = hidden)
   int kb[2];      // k-blocks of the first and of the second sum
   int tiles_m, tiles_n;
-  int first;      // number of its first tile in the launch
+  int first;      // number of its first unit in the launch: a tile, or one slice of a tile's sum
+  int slices, per;  // slices of the sum, k-blocks of one
+  float* part;      // slices > 1: [slice][32 rows of C][32 columns of C] blocks of partial sums
   int a_mn, b_mn;
   uint32_t idesc;
   int tma_store;
@@ -62,7 +65,7 @@ struct PairMaps {
 template <int N>
 struct PairArgs {
   PairProduct p[N];
-  int tiles;      // of all products
+  int units;      // of all products
   int out_type;   // asd_type
   int gelu;
   uint8_t* kept;
@@ -157,8 +160,9 @@ __device__ __forceinline__ void stage_half(uint8_t* buf, int lane, int half, con
   for (int i = 0; i < 4; ++i) stage_put(buf, lane, 4 * half + i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
 }
 
+// A unit of a launch: a tile, or the slice [kb0, kb1) of its sum.
 struct Tile {
-  int product, m0, n0;
+  int product, m0, n0, slice, kb0, kb1;
 };
 template <int BN, int N>
 __device__ __forceinline__ Tile tile_at(const PairArgs<N>& g, int t) {
@@ -168,11 +172,33 @@ __device__ __forceinline__ Tile tile_at(const PairArgs<N>& g, int t) {
     if (t >= g.p[i].first) r.product = i;
   const PairProduct& p = g.p[r.product];
   t -= p.first;
+  const int tiles = p.tiles_m * p.tiles_n;
+  r.slice = p.slices > 1 ? t / tiles : 0;  // the tiles of one slice are in flight together
+  t -= r.slice * tiles;
+  r.kb0 = r.slice * p.per;
+  r.kb1 = min(r.kb0 + p.per, p.kb[0] + p.kb[1]);
   const int band = t / (kBand * p.tiles_n), first = band * kBand;
   const int rows = min(p.tiles_m - first, kBand), in = t - first * p.tiles_n;
   r.m0 = (first + in % rows) * 2 * BM;
   r.n0 = (in / rows) * BN;
   return r;
+}
+
+// 64 columns of a warp's 32 rows of partial sums, as two blocks: float4 number `i` of row `lane` at 32 i + lane, so that both
+// this store and the load of join_kernel are contiguous over the lanes.
+__device__ __forceinline__ void part_out(const PairProduct& p, int slice, int row0, int col0, uint32_t acc, int lane) {
+  const int blocks_m = (p.m + 31) / 32, blocks_n = (p.n + 31) / 32;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t r[32];
+    tc_ld32(acc + 32 * h, r);
+    tc_wait_ld();
+    if (row0 >= p.m || col0 + 32 * h >= p.n) continue;
+    const int64_t block = ((int64_t)slice * blocks_m + row0 / 32) * blocks_n + col0 / 32 + h;
+    uint4* to = reinterpret_cast<uint4*>(p.part + block * kPartBlock) + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) to[32 * i] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+  }
 }
 
 template <int BN, int EPI>
@@ -200,7 +226,7 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
-  const int n_tiles = g.tiles;
+  const int n_tiles = g.units;
 
   if (threadIdx.x == 0) {
     prefetch_tmap(&maps.p[0].a[0]);
@@ -240,11 +266,10 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
         const Tile tile = tile_at<CN>(g, t);
         const PairProduct& p = g.p[tile.product];
         const auto& mp = maps.p[tile.product];
-        const int num_kb = p.kb[0] + p.kb[1];
         const bool a_mn = p.a_mn, b_mn = p.b_mn;
         const int m0 = tile.m0 + (int)rank * BM;
         const int n0 = EPI == OPS_GATE ? tile.n0 : tile.n0 + (int)rank * (BN / 2);
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
           const int part = kb >= p.kb[0] ? 1 : 0;
           const int k0 = (kb - part * p.kb[0]) * (I8 ? 128 : 64);
           const CUtensorMap* ma = &mp.a[part];
@@ -281,8 +306,8 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
       uint32_t phase = 0;
       int it = 0;
       for (int t = pair; t < n_tiles; t += n_pairs, ++it) {
-        const PairProduct& p = g.p[tile_at<CN>(g, t).product];
-        const int num_kb = p.kb[0] + p.kb[1];
+        const Tile tile = tile_at<CN>(g, t);
+        const PairProduct& p = g.p[tile.product];
         const bool a_mn = p.a_mn, b_mn = p.b_mn;
         const uint64_t step_a = desc_step(a_mn), step_b = desc_step(b_mn);
         const uint32_t idesc = p.idesc;
@@ -291,14 +316,14 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
         mbar_wait(acce_bar(acc), acc_phase ^ 1u, dead, g.err);  // both CTAs' epilogues have drained it
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
           mbar_wait(full_bar(stage), phase, dead, g.err);
           tc_fence_after();
           const uint32_t sa = tiles + stage * C::kStageBytes;
           const uint64_t da = smem_desc(sa, a_mn), db = smem_desc(sa + BM * 128, b_mn);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            tc_mma<I8, 2>(d_tmem, da + step_a * k, db + step_b * k, idesc, (kb | k) != 0 ? 1u : 0u);
+            tc_mma<I8, 2>(d_tmem, da + step_a * k, db + step_b * k, idesc, kb > tile.kb0 || k > 0 ? 1u : 0u);
           tc_commit_pair(empty_bar(stage));                 // frees the stage in this CTA ...
           tc_commit_pair(map_to_cta(empty_bar(stage), 1));  // ... and in the peer
           if (++stage == S) {
@@ -353,7 +378,9 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
           const int c0 = (half * kMine + u) * 64;  // column in the tile
           const int col0 = tile.n0 + c0;
           const bool any = rows_any && col0 < n;
-          if (EPI == OPS_STORE || EPI == OPS_GATE) {
+          if (EPI == OPS_STORE && p.part) {
+            part_out(p, tile.slice, row0, col0, t0 + c0, lane);
+          } else if (EPI == OPS_STORE || EPI == OPS_GATE) {
             if (tma) out.free();
             uint8_t* const buf = out.buf();
 #pragma unroll
@@ -496,6 +523,49 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
   }
 }
 
+// Joins the slices of sums, a block of 32 x 32 outputs to a block of threads: the partial sums in the order of the slices
+// (the same bits in every run), rounded once.
+struct JoinArgs {
+  struct One {
+    const float* part;
+    uint16_t* c;
+    int64_t ldc;
+    int m, n, slices, first;  // number of its first block
+  } p[kMostProducts];
+  int f16;
+};
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinArgs g) {
+  __shared__ float tile[32][33];
+  int j = 0;
+  for (int i = 1; i < kMostProducts; ++i)
+    if ((int)blockIdx.x >= g.p[i].first) j = i;
+  const JoinArgs::One& p = g.p[j];
+  const int block = (int)blockIdx.x - p.first, blocks_n = (p.n + 31) / 32;
+  const int64_t slice = (int64_t)((p.m + 31) / 32) * blocks_n * (kPartBlock / 4);
+  const float4* from = reinterpret_cast<const float4*>(p.part + (int64_t)block * kPartBlock) + threadIdx.x;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int i = 0; i < p.slices; ++i) {
+    const float4 v = from[i * slice];
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  float* put = &tile[threadIdx.x & 31][4 * (threadIdx.x >> 5)];
+  put[0] = s.x, put[1] = s.y, put[2] = s.z, put[3] = s.w;
+  __syncthreads();
+  const int r = threadIdx.x >> 3, c = 4 * (threadIdx.x & 7);
+  const int row = block / blocks_n * 32 + r, col = block % blocks_n * 32 + c;
+  if (row >= p.m || col >= p.n) return;
+  uint16_t* to = p.c + row * p.ldc + col;
+  const float* y = &tile[r][c];
+  if (col + 4 <= p.n && ((uintptr_t)to & 7) == 0) {
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack16(y[0], y[1], g.f16), pack16(y[2], y[3], g.f16));
+  } else {
+    for (int e = 0; e < min(4, p.n - col); ++e) to[e] = round16(y[e], g.f16);
+  }
+}
+
 // ---- host side --------------------------------------------------------------------------------
 
 CUtensorMapDataType map_type(int type) {
@@ -531,7 +601,7 @@ asd_status launch_pair(const asd_ops* o, const OpsGemm* list, int count, cudaStr
   memset(&maps, 0, sizeof(maps));
   PairArgs<N> g{};
   const int ke = I8 ? 128 : 64;
-  int64_t tiles = 0;
+  int64_t units = 0;
   for (int j = 0; j < N; ++j) {
     PairProduct& p = g.p[j];
     p.first = INT_MAX;
@@ -542,8 +612,11 @@ asd_status launch_pair(const asd_ops* o, const OpsGemm* list, int count, cudaStr
     p.kb[1] = q.parts == 2 ? (int)((q.k[1] + ke - 1) / ke) : 0;
     p.tiles_m = (int)((q.m + 2 * BM - 1) / (2 * BM));
     p.tiles_n = (int)((q.n + CN - 1) / CN);
-    p.first = (int)tiles;
-    tiles += (int64_t)p.tiles_m * p.tiles_n;
+    p.first = (int)units;
+    p.slices = std::max(1, q.slices);
+    p.per = (p.kb[0] + p.kb[1] + p.slices - 1) / p.slices;
+    p.part = p.slices > 1 ? q.part : nullptr;
+    units += (int64_t)p.tiles_m * p.tiles_n * p.slices;
     p.a_mn = q.a[0].mn, p.b_mn = q.b[0].mn;
     const uint32_t fmt = I8 ? 1u : (q.type == ASD_TYPE_BF16 ? 1u : 0u);  // signed 8-bit; bf16 or fp16
     p.idesc = (I8 ? 2u << 4 : 1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
@@ -561,14 +634,14 @@ asd_status launch_pair(const asd_ops* o, const OpsGemm* list, int count, cudaStr
     if (!ok) return ops_fail(ASD_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   }
   const OpsGemm& q = list[0];
-  g.tiles = (int)tiles;
+  g.units = (int)units;
   g.out_type = q.type;
   g.gelu = q.act == ASD_ACT_GELU;
   g.kept = q.kept;
   g.kept_cols = (int)((q.n + 31) / 32);
   g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias;
   g.err = o->err;
-  const int pairs = (int)std::min<int64_t>(tiles, o->num_sms / 2);
+  const int pairs = (int)std::min<int64_t>(units, o->num_sms / 2);
   ops_launch(op_pair_kernel<BN, EPI>, dim3(2 * pairs), dim3(kPairThreads), (size_t)C::kSmemBytes, st, 1, maps, g);
   return ops_launched("matrix product");
 }
@@ -592,9 +665,10 @@ double list_clocks(const asd_ops* o, const OpsGemm* list, int count, int bn) {
   std::fill(more, more + units, 0.0);
   int next = 0;  // the cluster that the next product's first tile goes to
   for (int j = 0; j < count; ++j) {
-    const int64_t tiles = pair_tiles(list[j], bn);
+    const int slices = std::max(1, list[j].slices);
+    const int64_t tiles = pair_tiles(list[j], bn) * slices;
     const int rest = (int)(tiles % units);
-    const double t = pair_kblocks(list[j]) * kblock_clocks(bn);
+    const double t = (double)((pair_kblocks(list[j]) + slices - 1) / slices) * kblock_clocks(bn);
     every += t * (double)(tiles / units);
     if (count == 1) return every + (rest ? t : 0.0) + 10700.0;
     for (int i = 0; i < rest; ++i) {
@@ -626,6 +700,23 @@ bool better_split(const asd_ops* o, const OpsGemm& q, bool early, SplitPlan* pla
   *plan = plan_split(o, q, early);
   return plan->clocks < std::min(list_clocks(o, &q, 1, 256), list_clocks(o, &q, 1, 128));
 }
+
+asd_status launch_join(const OpsGemm* list, int count, cudaStream_t st) {
+  JoinArgs g{};
+  int64_t blocks = 0;
+  int n = 0;
+  for (int j = 0; j < count; ++j) {
+    const OpsGemm& q = list[j];
+    if (q.slices <= 1) continue;
+    g.p[n++] = {q.part, (uint16_t*)q.c[0], q.ldc, (int)q.m, (int)q.n, q.slices, (int)blocks};
+    blocks += (q.m + 31) / 32 * ((q.n + 31) / 32);
+  }
+  if (n == 0) return ASD_OK;
+  for (int j = n; j < kMostProducts; ++j) g.p[j].first = INT_MAX;
+  g.f16 = list[0].type == ASD_TYPE_F16;
+  ops_launch(join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, 1, g);
+  return ops_launched("join of a sum's slices");
+}
 }  // namespace
 
 asd_status ops_gemm(const asd_ops* o, const OpsGemm& q, bool early, cudaStream_t st) {
@@ -650,7 +741,29 @@ asd_status ops_gemm_list(const asd_ops* o, const OpsGemm* list, int count, cudaS
     if (s != ASD_OK) return s;
     ++list, --count;
   }
-  return count ? launch_width<OPS_STORE>(o, list, count, st) : ASD_OK;
+  if (!count) return ASD_OK;
+  const asd_status s = launch_width<OPS_STORE>(o, list, count, st);
+  return s == ASD_OK ? launch_join(list, count, st) : s;
+}
+
+// The gradient of a narrow weight is a few tiles with a sum over all rows, which a few pairs would walk along while the
+// others are idle.  Up to a sixth of the pairs' number of tiles are therefore cut into as many slices as there are pairs, of
+// 16 k-blocks at least.  All gradients of the gated MLP, with slices against without: 32768 x 256 x 512 (2 tiles) 96 us
+// against 228, 131072 x 256 x 1024 (4) 565 against 1115, 32768 x 512 x 1280 (10) 273 against 356, 4096 x 512 x 1536 (12) 65
+// against 62.  Beyond that the input's gradient in the same launch keeps the pairs busy and the partial sums only cost: 4096 x
+// 512 x 2048 (16) 80 against 70, 8192 x 768 x 2048 (24) 184 against 167.  It goes by the sizes of the one product alone, so
+// that a gradient has the same bits whichever others are asked for.
+int sum_slices(const asd_ops* o, int64_t m, int64_t n, int64_t k) {
+  const int pairs = o->num_sms / 2;
+  const int64_t tiles = ((m + 255) / 256) * ((n + 255) / 256), kb = (k + 63) / 64;
+  if (6 * tiles > pairs) return 1;
+  const int64_t slices = std::min<int64_t>(pairs / tiles, kb / 16);
+  if (slices < 2) return 1;
+  const int64_t per = (kb + slices - 1) / slices;
+  return (int)((kb + per - 1) / per);
+}
+int64_t part_bytes(int64_t m, int64_t n, int slices) {
+  return slices > 1 ? (m + 31) / 32 * ((n + 31) / 32) * slices * (kPartBlock * 4) : 0;
 }
 
 asd_status ops_gemm_prepare() {

@@ -89,6 +89,8 @@ struct OpsGemm {
   Operand a[2], b[2];  // OPS_GATE: b[0] the gate's weights, b[1] the value's
   void* c[2];          // outputs; OPS_GATE: c[0] = h; OPS_GATE_GRAD: c[0] = dg, c[1] = du
   int64_t ldc;
+  int slices;          // ops_gemm_list: > 1: the sum in that many slices, through `part` (part_bytes)
+  float* part;
   uint8_t* kept;       // OPS_GATE: where the gate's two factors are kept, or NULL; OPS_GATE_GRAD: where they were
   const float* scale_a;  // OPS_I8
   const float* scale_b;
@@ -100,6 +102,9 @@ asd_status ops_gemm(const asd_ops* o, const OpsGemm& g, bool early, cudaStream_t
 // Up to four independent OPS_STORE products of one type.
 constexpr int kMostProducts = 4;
 asd_status ops_gemm_list(const asd_ops* o, const OpsGemm* g, int n, cudaStream_t st);
+// Slices of the sum that are worth their partial sums (1: none), and the bytes of these.
+int sum_slices(const asd_ops* o, int64_t m, int64_t n, int64_t k);
+int64_t part_bytes(int64_t m, int64_t n, int slices);
 asd_status ops_gemm_prepare();  // per device: opt-in to large shared memory
 
 // ---- asd_ops_stream.cu: matrix products of few rows ---------------------------------------------------

@@ -308,7 +308,7 @@ def mlp64(x, dy, w_in, w_out, act, t):
     out = {}
     y = h @ wo.T
     out["y"] = (y, y.abs() * u16 + (e_h + (h.abs() + e_h) * GAMMA(h_)) @ wo.abs().T * (1 + u16) + LEAST[t])
-    # backward, from g and u kept in 24 bits
+    # backward, from the gate's factors kept in 24 bits: the bound is that of g and u themselves kept so, which is wider
     k_g, k_u = e_g + (g.abs() + e_g) * 2.0 ** -15, e_u + (u.abs() + e_u) * 2.0 ** -15
     dh = dy @ wo
     e_dh = (dy.abs() @ wo.abs()) * GAMMA(width)
@@ -361,6 +361,23 @@ def test_gated_mlp_strides_and_parts(ops, rows):
             assert torch.equal(a, b) if n else a is None
     x3 = x.reshape(1, rows, width)
     assert torch.equal(ops.gated_mlp(x3, wi, wo)[0], ops.gated_mlp(x, wi, wo))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,width,hidden", [(1023, 8, 16), (1985, 40, 31), (2048, 64, 128), (2049, 257, 96), (9999, 520, 1000), (16500, 33, 31),
+                                               (20000, 100, 333), (40000, 512, 1280), (65537, 16, 8)])
+def test_weight_gradients_of_many_rows(ops, rows, width, hidden, kind):
+    """Sums over all rows with few outputs, which are cut into slices: each gradient, and its bits asked for alone and again."""
+    t = TYPES[kind]
+    x, dy, wi, wo = mlp_data(rows, width, hidden, t)
+    want = mlp64(x, dy, wi, wo, "silu", t)
+    _, saved = ops.gated_mlp_forward(x, wi, wo)
+    got = ops.gated_mlp_backward(dy, x, wi, wo, saved)
+    for name, g in zip(("dx", "dw_in", "dw_out"), got):
+        within(g, *want[name], name)
+    for _ in range(3):
+        assert torch.equal(ops.gated_mlp_backward(dy, x, wi, wo, saved, need=(False, True, False))[1], got[1])
+        assert torch.equal(ops.gated_mlp_backward(dy, x, wi, wo, saved, need=(False, False, True))[2], got[2])
 
 
 def test_gated_mlp_gradient_against_differences(ops):
