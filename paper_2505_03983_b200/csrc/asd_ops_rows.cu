@@ -1047,8 +1047,12 @@ void grad_t(const asd_ops* o, const NormGradArgs& n, cudaStream_t st) {
   else if (n.width <= kGradWidth)
     ops_launch(rmsnorm_grad_kernel<T, VEC, 512, 16>, dim3(n.blocks), dim3(512), grad_bytes<T, VEC, 512>(n), st, 1, n);
   else {
-    ops_launch(rmsnorm_grad_long_kernel<T>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    NormGradArgs stats = n;
+    stats.dx = nullptr;
+    const bool over_dy = n.part && n.dx == n.dy;  // dw needs dy, so dx comes after it
+    ops_launch(rmsnorm_grad_long_kernel<T>, dim3(n.rows), dim3(512), 0, st, 1, over_dy ? stats : n);
     if (n.part) ops_launch(columns_dw_kernel<T>, dim3((n.width + 127) / 128, n.blocks), dim3(128), 0, st, 1, n);
+    if (over_dy) ops_launch(rmsnorm_grad_long_kernel<T>, dim3(n.rows), dim3(512), 0, st, 1, n);
   }
 }
 

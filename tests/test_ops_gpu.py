@@ -176,6 +176,27 @@ def test_norm_in_place_sum_and_strides(ops, width):
             assert torch.isnan(whole[:, :off]).all() and torch.isnan(whole[:, off + width:]).all()  # nothing beside the rows
 
 
+@pytest.mark.parametrize("rows,width", [(6, 64), (700, 33), (6, 1000), (1500, 1001), (6, 5000), (6, 9000), (6, 17003)])
+def test_norm_gradient_in_place(ops, rows, width):
+    """Through the C ABI: dx may be stored over dy or over ds, with dw as if it were not."""
+    import ctypes as C
+    from paper_2505_03983_b200 import operators as o
+    t = torch.bfloat16
+    s, dy, ds, w = rand((rows, width), 1, t), rand((rows, width), 2, t), rand((rows, width), 4, t), rand((width,), 3, t)
+    dx, dw = ops.add_rmsnorm_backward(dy, s, w, ds=ds)
+    for over in ("dy", "ds"):
+        v = {"dy": dy.clone(), "ds": ds.clone()}
+        got = torch.empty_like(dw)
+        a = o._NormBackward(rows=rows, width=width, type=2, w_type=2, eps=1e-6, dy=v["dy"].data_ptr(), ld_dy=width, s=s.data_ptr(), ld_s=width,
+                            ds=v["ds"].data_ptr(), ld_ds=width, weight=w.data_ptr(), dx=v[over].data_ptr(), ld_dx=width, dw=got.data_ptr())
+        n = C.c_int64()
+        assert ops.lib.asd_add_rmsnorm_backward_workspace(ops._handle, C.byref(a), C.byref(n)) == 0
+        space = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+        a.workspace, a.workspace_bytes = space.data_ptr(), n.value
+        assert ops.lib.asd_add_rmsnorm_backward(ops._handle, C.byref(a), torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(v[over], dx) and torch.equal(got, dw), over
+
+
 def test_norm_rows_that_cannot_be_represented(ops):
     x = rand((6, 640), 1, torch.float32)
     x[1, 5], x[2, 7], x[3, 9] = float("nan"), float("inf"), -float("inf")
