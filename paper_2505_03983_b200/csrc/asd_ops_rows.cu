@@ -4,10 +4,10 @@
 //
 // All of them are bound by memory: a row is read once, kept in registers over its reductions, and written once.  A row
 // belongs to 32, 128, 256 or 512 threads (rows of up to 1024, 4096, 8192, 16384), 32 elements to a thread, so that a thread has its
-// 16-byte loads in flight together; longer rows are read a second time.  Rows whose address, distance or length is not a
-// multiple of 8 elements come into shared memory in the aligned 16-byte pieces that hold them, one row ahead, and are read
-// from there element by element, neighbouring threads on neighbouring elements (read so from memory, 6001 rows of 2 x 2477
-// bf16 took 127 us to quantise).
+// 16-byte loads in flight together; longer rows are read a second time, and several narrow ones (up to 256) share a warp.
+// Rows of more than 256 whose address, distance or length is not a multiple of 8 elements come into shared memory in the aligned
+// 16-byte pieces that hold them, one row ahead, and are read from there element by element, neighbouring threads on neighbouring
+// elements (read so from memory, 6001 rows of 2 x 2477 bf16 took 127 us to quantise).
 //
 // Measured (of 6.55 TB/s): norm 8192 x 4096 bf16 43 us = 6.2 TB/s, to int8 32768 x 1024 42.6 us = 5.5 TB/s, gradient 8192 x 4096 52 us =
 // 5.2 TB/s, gate to int8 8192 x 8192 56.6 us = 5.9 TB/s.  One row of 4096 takes 4 us, a kernel's start and end.
@@ -886,6 +886,220 @@ __global__ void __launch_bounds__(1024) reduce_dw_kernel(const float* part, int 
   if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < width) dw[blockIdx.x * 32 + threadIdx.y] = from_f<W>(v);
 }
 
+// ---- narrow rows: up to 256 elements ----
+// A row belongs to L = 8, 16 or 32 lanes with kNarrow elements each, so that a warp works on 32 / L rows at once and its sums
+// are a few shuffles.  Lane `t` has the elements 8 t .. 8 t + 7 of rows in 16-byte pieces (VEC = 8), or t, t + L, ... of any
+// others (VEC = 1), which neighbouring lanes read from the same sectors.
+// Measured in bf16, with a warp to a row and 32 elements to a lane in brackets (a row of 64 then costs the instructions of
+// one of 1024): 1048576 x 64 norm 89 us (391), to int8 107 (473), gradient 97 (824), to int8 without the norm 47 (231); these move
+// 537, 470, 537 and 206 MB.  131072 x 100, rows that do not start on 16 bytes: 27 (115), 36 (188), 43 (171), 19 (84).
+constexpr int kNarrow = 8;
+constexpr int kNarrowWidth = 32 * kNarrow;
+constexpr int kNarrowBlock = 128;       // of the norm and its gradient
+constexpr int kNarrowQuantBlock = 256;  // 1048576 x 64: 47 us, 68 with 128, which leave before the next one starts
+
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+template <int L>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+#pragma unroll
+  for (int o = L / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+template <int VEC, int L>
+__device__ __forceinline__ int narrow_column(int t, int i) { return VEC == 8 ? kNarrow * t + i : t + L * i; }
+// A lane's elements of a row; those beyond its end, and of a row that is not there, are zero.
+template <int VEC, int L, typename T>
+__device__ __forceinline__ void narrow_load(const T* p, int width, int t, bool live, float (&f)[kNarrow]) {
+#pragma unroll
+  for (int i = 0; i < kNarrow; ++i) f[i] = 0.f;
+  if constexpr (VEC == 8) {
+    if (live && kNarrow * t < width) load_vec<8, T>(p + kNarrow * t, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kNarrow; ++i)
+      if (live && t + L * i < width) f[i] = to_f<T>(p[t + L * i]);
+  }
+}
+template <int VEC, int L, typename T>
+__device__ __forceinline__ void narrow_store(T* p, int width, int t, const float (&f)[kNarrow]) {
+  if constexpr (VEC == 8) {
+    if (kNarrow * t < width) store_vec<8, T>(p + kNarrow * t, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kNarrow; ++i)
+      if (t + L * i < width) p[t + L * i] = from_f<T>(f[i]);
+  }
+}
+template <int VEC, int L>
+__device__ __forceinline__ void narrow_put_q(int8_t* p, int width, int t, const float (&f)[kNarrow], const RowScale& rs) {
+  if constexpr (VEC == 8) {
+    if (kNarrow * t < width) put_q<8>(p + kNarrow * t, f, rs);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kNarrow; ++i)
+      if (t + L * i < width) p[t + L * i] = rs.ok ? (int8_t)rounded_bits(f[i], rs.inv) : (int8_t)0;
+  }
+}
+template <int VEC, int L, typename T>
+__device__ __forceinline__ void narrow_weight(const void* w, int w_f32, int width, int t, float (&f)[kNarrow]) {
+  if (!w) {
+#pragma unroll
+    for (int i = 0; i < kNarrow; ++i) f[i] = 1.f;
+  } else if (w_f32) {
+    narrow_load<VEC, L, float>(reinterpret_cast<const float*>(w), width, t, true, f);
+  } else {
+    narrow_load<VEC, L, T>(reinterpret_cast<const T*>(w), width, t, true, f);
+  }
+}
+
+template <typename T, int VEC, int L, bool Q8>
+__global__ void __launch_bounds__(kNarrowBlock) narrow_norm_kernel(const NormArgs a) {
+  dep_wait();
+  dep_launch();
+  const int t = threadIdx.x % L;
+  const int64_t row = (int64_t)blockIdx.x * (kNarrowBlock / L) + threadIdx.x / L;
+  const bool live = row < a.rows;  // the lanes of rows beyond the last take part in the shuffles
+  float f[kNarrow], w[kNarrow];
+  narrow_load<VEC, L, T>(reinterpret_cast<const T*>(a.x) + row * a.ld_x, a.width, t, live, f);
+  if (a.r) {
+    float r[kNarrow];
+    narrow_load<VEC, L, T>(reinterpret_cast<const T*>(a.r) + row * a.ld_r, a.width, t, live, r);
+#pragma unroll
+    for (int i = 0; i < kNarrow; ++i) f[i] = to_f<T>(from_f<T>(f[i] + r[i]));
+  }
+  narrow_weight<VEC, L, T>(a.w, a.w_f32, a.width, t, w);
+  if (a.sum && live) narrow_store<VEC, L, T>(reinterpret_cast<T*>(a.sum) + row * a.ld_s, a.width, t, f);
+  float sq = 0.f;
+#pragma unroll
+  for (int i = 0; i < kNarrow; ++i) sq = fmaf(f[i], f[i], sq);
+  sq = group_sum<L>(sq);
+  const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kNarrow; ++i) {
+    // elements beyond the row's end are not there to make 0 inf of
+    f[i] = narrow_column<VEC, L>(t, i) < a.width ? f[i] * rho * w[i] : 0.f;
+    if (Q8) most = max(most, mag(f[i]));
+  }
+  if (!Q8) {
+    if (live) narrow_store<VEC, L, T>(reinterpret_cast<T*>(a.y) + row * a.ld_y, a.width, t, f);
+  } else {
+    const RowScale rs = row_scale(group_max<L>(most));
+    if (!live) return;
+    narrow_put_q<VEC, L>(reinterpret_cast<int8_t*>(a.y) + row * a.ld_y, a.width, t, f, rs);
+    if (t == 0) a.scale[row] = rs.scale;
+  }
+}
+
+template <typename T, int VEC, int L>
+__global__ void __launch_bounds__(kNarrowQuantBlock) narrow_quantize_kernel(const QuantArgs a) {
+  dep_wait();
+  dep_launch();
+  const int t = threadIdx.x % L;
+  const int64_t row = (int64_t)blockIdx.x * (kNarrowQuantBlock / L) + threadIdx.x / L;
+  const bool live = row < a.rows;
+  const T* x = reinterpret_cast<const T*>(a.x) + row * a.ld_x;
+  float f[kNarrow];
+  narrow_load<VEC, L, T>(x, a.width, t, live, f);
+  if (a.act != ASD_ACT_NONE) {
+    float u[kNarrow];
+    narrow_load<VEC, L, T>(x + a.width, a.width, t, live, u);
+#pragma unroll
+    for (int i = 0; i < kNarrow; i += 2) {
+      const float2 h = gated2(make_float2(f[i], f[i + 1]), make_float2(u[i], u[i + 1]), a.act);
+      f[i] = h.x;
+      f[i + 1] = h.y;
+    }
+  }
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kNarrow; ++i) most = max(most, mag(f[i]));
+  const RowScale rs = row_scale(group_max<L>(most));
+  if (!live) return;
+  narrow_put_q<VEC, L>(a.q + row * a.ld_q, a.width, t, f, rs);
+  if (t == 0) a.scale[row] = rs.scale;
+}
+
+// A block walks over its rows, kNarrowBlock / L at once and two such steps with their loads in flight together; the sums of dw stay
+// in a lane's registers and are joined over the block's row groups at the end.
+template <typename T, int VEC, int L>
+__global__ void __launch_bounds__(kNarrowBlock) narrow_grad_kernel(const NormGradArgs a) {
+  constexpr int ROWS = kNarrowBlock / L, U = VEC == 8 ? 2 : 1;
+  __shared__ float sums[kNarrowBlock / 32][kNarrowWidth];
+  dep_wait();
+  dep_launch();
+  const int t = threadIdx.x % L;
+  float w[kNarrow], acc[kNarrow];
+  narrow_weight<VEC, L, T>(a.w, a.w_f32, a.width, t, w);
+#pragma unroll
+  for (int i = 0; i < kNarrow; ++i) {
+    if (narrow_column<VEC, L>(t, i) >= a.width) w[i] = 0.f;
+    acc[i] = 0.f;
+  }
+  for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += (int64_t)a.blocks * ROWS * U) {
+    float f[U][kNarrow], g[U][kNarrow], e[U][kNarrow];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = first + (int64_t)u * a.blocks * ROWS + threadIdx.x / L;
+      const bool live = row < a.rows;
+      narrow_load<VEC, L, T>(reinterpret_cast<const T*>(a.s) + row * a.ld_s, a.width, t, live, f[u]);
+      narrow_load<VEC, L, T>(reinterpret_cast<const T*>(a.dy) + row * a.ld_dy, a.width, t, live, g[u]);
+      narrow_load<VEC, L, T>(reinterpret_cast<const T*>(a.ds) + row * a.ld_ds, a.width, t, live && a.ds, e[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = first + (int64_t)u * a.blocks * ROWS + threadIdx.x / L;
+      const bool live = row < a.rows;
+      float sq = 0.f, dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < kNarrow; ++i) {
+        sq = fmaf(f[u][i], f[u][i], sq);
+        dot = fmaf(g[u][i] * w[i], f[u][i], dot);
+      }
+      sq = group_sum<L>(sq);
+      dot = group_sum<L>(dot);
+      const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
+      const float k = -(rho * dot / (float)a.width) * rho * rho;
+#pragma unroll
+      for (int i = 0; i < kNarrow; ++i) {
+        if (live) acc[i] = fmaf(g[u][i], f[u][i] * rho, acc[i]);
+        e[u][i] = fmaf(f[u][i], k, fmaf(g[u][i] * w[i], rho, e[u][i]));
+      }
+      if (live) narrow_store<VEC, L, T>(reinterpret_cast<T*>(a.dx) + row * a.ld_dx, a.width, t, e[u]);
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int i = 0; i < kNarrow; ++i) {
+    for (int o = L; o < 32; o <<= 1) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
+    if ((threadIdx.x & 31) < L) sums[threadIdx.x >> 5][narrow_column<VEC, L>(t, i)] = acc[i];
+  }
+  __syncthreads();
+  for (int col = threadIdx.x; col < a.width; col += kNarrowBlock) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kNarrowBlock / 32; ++k) v += sums[k][col];
+    a.part[(size_t)blockIdx.x * a.width + col] = v;
+  }
+}
+
+// Calls f with the lanes of a narrow row as a constant.
+template <typename F>
+void with_lanes(int width, F f) {
+  if (width <= 8 * kNarrow)
+    f(std::integral_constant<int, 8>());
+  else if (width <= 16 * kNarrow)
+    f(std::integral_constant<int, 16>());
+  else
+    f(std::integral_constant<int, 32>());
+}
+unsigned narrow_grid(int rows, int lanes, int block) { return (unsigned)(((int64_t)rows * lanes + block - 1) / block); }
+
 // Up to four matrices to rows of a multiple of 16 bytes, in one launch (blockIdx.y).  A thread makes 16 bytes of a row from
 // the aligned words that hold them, each shifted by the row's misalignment; a row's last bytes, and elements of a row that
 // does not start on a word, are read one by one where a word would reach outside the row.
@@ -935,7 +1149,7 @@ bool aligned(const void* p, int64_t ld, int es, int bytes) { return ((uintptr_t)
 // Threads to a row.  A row of up to 1024 is a warp's, so that its sums need no barrier, unless there are too few rows to
 // fill the SMs with warps; then, and beyond, a block's.
 int row_threads(const asd_ops* o, int64_t rows, int width) {
-  if (width <= 32 * kPer && (width <= 256 || rows >= 8 * o->num_sms)) return 32;
+  if (width <= 32 * kPer && rows >= 8 * o->num_sms) return 32;
   if (width <= 128 * kPer && (width <= 1024 || rows >= 4 * o->num_sms)) return 128;
   if (width <= 256 * kPer && rows >= 2 * o->num_sms) return 256;
   return 512;
@@ -967,6 +1181,13 @@ void rmsnorm_staged(const asd_ops* o, const NormArgs& n, cudaStream_t st) {
 }
 template <typename T, bool Q8>
 void rmsnorm_t(const asd_ops* o, const NormArgs& n, bool vec, cudaStream_t st) {
+  if (n.width <= kNarrowWidth) {
+    with_lanes(n.width, [&](auto lanes) {
+      constexpr int L = decltype(lanes)::value;
+      ops_launch(vec ? narrow_norm_kernel<T, 8, L, Q8> : narrow_norm_kernel<T, 1, L, Q8>, dim3(narrow_grid(n.rows, L, kNarrowBlock)), dim3(kNarrowBlock), 0, st, 1, n);
+    });
+    return;
+  }
   if (n.width > 512 * kPer) {
     if (vec)
       ops_launch(rmsnorm_kernel<T, 8, 512, Q8, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
@@ -1011,6 +1232,13 @@ void quantize_rows(const asd_ops* o, QuantArgs n, bool vec, cudaStream_t st) {
 }
 template <typename T>
 void quantize_t(const asd_ops* o, const QuantArgs& n, bool vec, cudaStream_t st) {
+  if (n.width <= kNarrowWidth) {
+    with_lanes(n.width, [&](auto lanes) {
+      constexpr int L = decltype(lanes)::value;
+      ops_launch(vec ? narrow_quantize_kernel<T, 8, L> : narrow_quantize_kernel<T, 1, L>, dim3(narrow_grid(n.rows, L, kNarrowQuantBlock)), dim3(kNarrowQuantBlock), 0, st, 1, n);
+    });
+    return;
+  }
   if (n.width > 512 * kPer) {
     if (vec)
       ops_launch(quantize_long_kernel<T, 8>, dim3(n.rows), dim3(512), 0, st, 1, n);
@@ -1030,6 +1258,10 @@ constexpr int kGradWidth = 8192;  // the longest row whose sums of dw a block ke
 // Blocks of the gradient: as many as the SMs hold together, so that each block's sums of dw are over as many rows as
 // possible.
 int grad_blocks(const asd_ops* o, int64_t rows, int width) {
+  if (width <= kNarrowWidth) {  // of several rows at once
+    const int64_t all = ((int64_t)narrow_grid((int)rows, width <= 64 ? 8 : width <= 128 ? 16 : 32, kNarrowBlock)), most = 5 * (int64_t)o->num_sms;
+    return (int)(all < most ? all : most);
+  }
   const int per_sm = width <= 1024 ? 8 : width <= 4096 ? 2 : width <= kGradWidth ? 1 : 2;
   const int64_t most = (int64_t)per_sm * o->num_sms;
   return (int)(rows < most ? rows : most);
@@ -1040,7 +1272,12 @@ size_t grad_bytes(const NormGradArgs& n) {
 }
 template <typename T, int VEC>
 void grad_t(const asd_ops* o, const NormGradArgs& n, cudaStream_t st) {
-  if (n.width <= 1024)
+  if (n.width <= kNarrowWidth)
+    with_lanes(n.width, [&](auto lanes) {
+      constexpr int L = decltype(lanes)::value;
+      ops_launch(narrow_grad_kernel<T, VEC, L>, dim3(n.blocks), dim3(kNarrowBlock), 0, st, 1, n);
+    });
+  else if (n.width <= 1024)
     ops_launch(rmsnorm_grad_kernel<T, VEC, 64, 16>, dim3(n.blocks), dim3(64), grad_bytes<T, VEC, 64>(n), st, 1, n);
   else if (n.width <= 4096)
     ops_launch(rmsnorm_grad_kernel<T, VEC, 256, 16>, dim3(n.blocks), dim3(256), grad_bytes<T, VEC, 256>(n), st, 1, n);

@@ -235,6 +235,36 @@ def test_quantize(ops, rows, width, kind, act):
     assert torch.equal(ops.quantize_i8(padded(x, 5, 3), act=act)[0], q) and torch.equal(ops.quantize_i8(padded(x, 8), act=act)[1], scale)
 
 
+# Rows that share a warp, by 4, 2 and 1, with rows missing in the last warp, and more of them than are worked on at once.
+NARROW_SHAPES = [(1, 2), (5, 63), (7, 64), (13, 65), (3, 128), (9, 129), (17, 200), (33, 254), (2, 256), (40001, 24), (30001, 64), (20003, 100), (9001, 256)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,width", NARROW_SHAPES)
+def test_narrow_rows(ops, rows, width, kind):
+    test_add_rmsnorm(ops, rows, width, kind)
+    test_add_rmsnorm_i8(ops, rows, width, kind)
+    test_add_rmsnorm_backward(ops, rows, width, kind)
+    for act in (None, "silu", "gelu"):
+        test_quantize(ops, rows, width, kind, act)
+
+
+@pytest.mark.parametrize("width", [24, 33, 64, 200])
+def test_narrow_rows_that_cannot_be_represented(ops, width):
+    """An infinity and a NaN stay in their rows, whose neighbours share the warp; rows of zeros with eps."""
+    x = rand((37, width), 1)
+    x[3], x[9, width // 2], x[20, 0] = 0.0, float("inf"), float("nan")
+    others = [i for i in range(37) if i not in (9, 20)]
+    y, _ = ops.add_rmsnorm(x, None)
+    assert torch.isfinite(y[others]).all() and torch.isnan(y[20]).all() and torch.isnan(y[9, width // 2])
+    q, scale, _ = ops.add_rmsnorm_i8(x, None)
+    assert not q[[3, 9, 20]].any() and torch.isnan(scale[[9, 20]]).all() and torch.isfinite(scale[others]).all()
+    q, scale = ops.quantize_i8(x)
+    assert not q[[3, 9, 20]].any() and torch.isnan(scale[[9, 20]]).all() and torch.isfinite(scale[others]).all()
+    dx, _ = ops.add_rmsnorm_backward(rand((37, width), 2), x, None)
+    assert torch.isfinite(dx[others]).all() and torch.isnan(dx[20]).all()
+
+
 def test_quantize_edges(ops):
     x = torch.zeros((5, 40), device="cuda")
     x[1], x[2, 3], x[3, 4] = 1e-38, float("inf"), float("nan")
