@@ -194,7 +194,8 @@ asd_status run_backward(const asd_ops* o, const asd_gated_mlp_backward_args* a, 
   }
   if (a->dw_in) {  // dg^T x, du^T x
     for (int i = 0; i < 2; ++i) {
-      OpsGemm& g = product({i ? du : dg, true}, {x, true}, (uint8_t*)a->dw_in + i * 2 * a->ld_dw_in * a->hidden, a->ld_dw_in, a->hidden, a->width, rows);
+      uint8_t* c = (uint8_t*)a->dw_in + i * 2 * a->ld_dw_in * a->hidden;
+      OpsGemm& g = product({i ? du : dg, true}, {x, true}, c, a->ld_dw_in, a->hidden, a->width, rows);
       g.slices = s_in, g.part = part_in[i];
     }
   }

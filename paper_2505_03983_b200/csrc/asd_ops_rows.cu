@@ -896,7 +896,7 @@ __global__ void __launch_bounds__(1024) reduce_dw_kernel(const float* part, int 
 constexpr int kNarrow = 8;
 constexpr int kNarrowWidth = 32 * kNarrow;
 constexpr int kNarrowBlock = 128;       // of the norm and its gradient
-constexpr int kNarrowQuantBlock = 256;  // 1048576 x 64: 47 us, 68 with 128, which leave before the next one starts
+constexpr int kNarrowQuantBlock = 256;  // 1048576 x 64: 47 us; with 128 threads 68, for blocks that end faster than they can be started
 
 template <int L>
 __device__ __forceinline__ float group_sum(float v) {
@@ -1184,7 +1184,8 @@ void rmsnorm_t(const asd_ops* o, const NormArgs& n, bool vec, cudaStream_t st) {
   if (n.width <= kNarrowWidth) {
     with_lanes(n.width, [&](auto lanes) {
       constexpr int L = decltype(lanes)::value;
-      ops_launch(vec ? narrow_norm_kernel<T, 8, L, Q8> : narrow_norm_kernel<T, 1, L, Q8>, dim3(narrow_grid(n.rows, L, kNarrowBlock)), dim3(kNarrowBlock), 0, st, 1, n);
+      ops_launch(vec ? narrow_norm_kernel<T, 8, L, Q8> : narrow_norm_kernel<T, 1, L, Q8>, dim3(narrow_grid(n.rows, L, kNarrowBlock)),
+                 dim3(kNarrowBlock), 0, st, 1, n);
     });
     return;
   }
@@ -1235,7 +1236,8 @@ void quantize_t(const asd_ops* o, const QuantArgs& n, bool vec, cudaStream_t st)
   if (n.width <= kNarrowWidth) {
     with_lanes(n.width, [&](auto lanes) {
       constexpr int L = decltype(lanes)::value;
-      ops_launch(vec ? narrow_quantize_kernel<T, 8, L> : narrow_quantize_kernel<T, 1, L>, dim3(narrow_grid(n.rows, L, kNarrowQuantBlock)), dim3(kNarrowQuantBlock), 0, st, 1, n);
+      ops_launch(vec ? narrow_quantize_kernel<T, 8, L> : narrow_quantize_kernel<T, 1, L>, dim3(narrow_grid(n.rows, L, kNarrowQuantBlock)),
+                 dim3(kNarrowQuantBlock), 0, st, 1, n);
     });
     return;
   }
