@@ -2,12 +2,38 @@
 
     y, s = add_rmsnorm(x, weight, residual)      y = norm(x + residual) * weight, s = x + residual
     y = gated_mlp(x, w_in, w_out, act)           y = (act(x Wg^T) * (x Wu^T)) w_out^T
+
+They have first derivatives only: a gradient that was made with create_graph=True raises where it is differentiated through one of
+these functions.
 """
 from __future__ import annotations
 
 import torch
 
 from .operators import default_ops
+
+
+class _FirstOnly(torch.autograd.Function):
+    """Gradients that were computed without a graph, tied to what they depend on by a derivative that raises.
+    torch.autograd.function.once_differentiable does so only where a gradient that comes in requires one itself, and so lets the
+    derivative of a fixed direction (a divergence) pass for a constant."""
+
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tuple(t.view_as(t) for t in tensors[:n])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("add_rmsnorm and gated_mlp have first derivatives only: differentiating their gradients is not supported")
+
+
+def _first_only(grads, *depend_on):
+    """grads (None among them), as a backward pass returns them."""
+    if not torch.is_grad_enabled():  # no create_graph
+        return grads
+    made = [g for g in grads if g is not None]
+    tied = iter(_FirstOnly.apply(len(made), *made, *(t for t in depend_on if t is not None)))
+    return tuple(None if g is None else next(tied) for g in grads)
 
 
 class _AddRmsnorm(torch.autograd.Function):
@@ -23,6 +49,7 @@ class _AddRmsnorm(torch.autograd.Function):
         s, weight = ctx.saved_tensors
         need_dw = weight is not None and ctx.needs_input_grad[1]
         dx, dw = default_ops().add_rmsnorm_backward(dy, s, weight, ds=ds, eps=ctx.eps, need_dweight=need_dw)
+        dx, dw = _first_only((dx, dw), s, weight, dy, ds)
         return dx, dw, dx if ctx.has_residual else None, None
 
 
@@ -39,7 +66,8 @@ class _GatedMlp(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, w_in, w_out, saved = ctx.saved_tensors
-        return (*default_ops().gated_mlp_backward(dy, x, w_in, w_out, saved, act=ctx.act, need=ctx.needs_input_grad[:3]), None)
+        grads = default_ops().gated_mlp_backward(dy, x, w_in, w_out, saved, act=ctx.act, need=ctx.needs_input_grad[:3])
+        return (*_first_only(grads, x, w_in, w_out, dy), None)
 
 
 def add_rmsnorm(x, weight, residual=None, eps=1e-6):
