@@ -55,9 +55,9 @@ class _AddRmsnorm(torch.autograd.Function):
 
 class _GatedMlp(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w_in, w_out, act):
+    def forward(ctx, x, w_in, w_out, act, keep):
         ctx.act = act
-        if not any(ctx.needs_input_grad):
+        if not keep:
             return default_ops().gated_mlp(x, w_in, w_out, act=act)
         y, saved = default_ops().gated_mlp_forward(x, w_in, w_out, act=act)
         ctx.save_for_backward(x, w_in, w_out, saved)
@@ -67,7 +67,7 @@ class _GatedMlp(torch.autograd.Function):
     def backward(ctx, dy):
         x, w_in, w_out, saved = ctx.saved_tensors
         grads = default_ops().gated_mlp_backward(dy, x, w_in, w_out, saved, act=ctx.act, need=ctx.needs_input_grad[:3])
-        return (*_first_only(grads, x, w_in, w_out, dy), None)
+        return (*_first_only(grads, x, w_in, w_out, dy), None, None)
 
 
 def add_rmsnorm(x, weight, residual=None, eps=1e-6):
@@ -77,4 +77,6 @@ def add_rmsnorm(x, weight, residual=None, eps=1e-6):
 
 def gated_mlp(x, w_in, w_out, act="silu"):
     """AsdOps.gated_mlp with gradients in x, w_in and w_out."""
-    return _GatedMlp.apply(x, w_in, w_out, act)
+    # in the function itself needs_input_grad would be true of a parameter under no_grad too
+    keep = torch.is_grad_enabled() and (x.requires_grad or w_in.requires_grad or w_out.requires_grad)
+    return _GatedMlp.apply(x, w_in, w_out, act, keep)

@@ -97,3 +97,27 @@ def test_first_derivatives_with_a_graph_are_the_same(stand, which):
     dz, = torch.autograd.grad(f(x).square().sum() + z.pow(3).sum(), z, create_graph=True)
     ddz, = torch.autograd.grad(dz.sum(), z)
     assert torch.allclose(ddz, 6 * z)
+
+
+@pytest.mark.parametrize("off", [torch.no_grad, torch.inference_mode])
+def test_serving_keeps_nothing_for_a_backward_pass(stand, off):
+    """Parameters that require gradients, in a region that records none: the forward that keeps nothing."""
+    x, wi, wo = leaves((5, 8), (12, 8), (8, 6))
+    with off():
+        y = autograd.gated_mlp(x, wi, wo)
+    assert stand.calls == [("gated_mlp",)] and not y.requires_grad
+    stand.calls.clear()
+    autograd.gated_mlp(x.detach(), wi.detach(), wo.detach())
+    assert stand.calls == [("gated_mlp",)]
+    stand.calls.clear()
+    autograd.gated_mlp(x.detach(), wi.detach(), wo).sum().backward()
+    assert stand.calls == [("gated_mlp_forward",), ("gated_mlp_backward", (False, False, True))]
+
+
+def test_forward_mode_raises(stand):
+    x, w, wi, wo = make(5, 8), make(8), make(12, 8), make(8, 6)
+    with torch.autograd.forward_ad.dual_level():
+        d = torch.autograd.forward_ad.make_dual(x, make(5, 8, seed=9))
+        for f in (lambda: autograd.gated_mlp(d, wi, wo), lambda: autograd.add_rmsnorm(d, w)):
+            with pytest.raises((RuntimeError, NotImplementedError)):
+                f()
