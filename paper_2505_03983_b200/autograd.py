@@ -41,6 +41,7 @@ class _AddRmsnorm(torch.autograd.Function):
     def forward(ctx, x, weight, residual, eps):
         y, s = default_ops().add_rmsnorm(x, weight, residual=residual, eps=eps)
         ctx.save_for_backward(s, weight)
+        ctx.set_materialize_grads(False)
         ctx.eps, ctx.has_residual = eps, residual is not None
         return y, s if residual is not None else s.view_as(s)  # without a residual s is x: an output of its own
 
@@ -48,6 +49,8 @@ class _AddRmsnorm(torch.autograd.Function):
     def backward(ctx, dy, ds):
         s, weight = ctx.saved_tensors
         need_dw = weight is not None and ctx.needs_input_grad[1]
+        if dy is None:  # only s was used
+            return ds, torch.zeros_like(weight) if need_dw else None, ds if ctx.has_residual else None, None
         dx, dw = default_ops().add_rmsnorm_backward(dy, s, weight, ds=ds, eps=ctx.eps, need_dweight=need_dw)
         dx, dw = _first_only((dx, dw), s, weight, dy, ds)
         return dx, dw, dx if ctx.has_residual else None, None

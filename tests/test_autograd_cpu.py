@@ -121,3 +121,24 @@ def test_forward_mode_raises(stand):
         for f in (lambda: autograd.gated_mlp(d, wi, wo), lambda: autograd.add_rmsnorm(d, w)):
             with pytest.raises((RuntimeError, NotImplementedError)):
                 f()
+
+
+def test_outputs_that_are_not_used_bring_no_zeros(stand):
+    """Where s, or y, is not used further its gradient is absent, not a tensor of zeros that a kernel reads."""
+    x, r, w = leaves((5, 8), (5, 8), (8,))
+    for residual in (None, r):
+        stand.calls.clear()
+        autograd.add_rmsnorm(x, w, residual)[0].square().sum().backward()
+        assert stand.calls[1:] == [("add_rmsnorm_backward", False, True)]
+    # s alone: its gradient is that of x and of the residual, and the weight's is zero
+    stand.calls.clear()
+    ds = make(5, 8, seed=9)
+    dx, dw, dr = torch.autograd.grad(autograd.add_rmsnorm(x, w, r)[1], (x, w, r), ds)
+    assert len(stand.calls) == 1 and torch.equal(dx, ds) and torch.equal(dr, ds) and not dw.any()
+    # both, against the formula's own graph
+    y, s = autograd.add_rmsnorm(x, w, r)
+    got = torch.autograd.grad((y.square().sum() + s.pow(3).sum()), (x, w, r))
+    s = x + r
+    y = s * torch.rsqrt(s.square().mean(-1, keepdim=True) + 1e-6) * w
+    for a, b in zip(got, torch.autograd.grad((y.square().sum() + s.pow(3).sum()), (x, w, r))):
+        assert torch.allclose(a, b)
