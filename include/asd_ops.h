@@ -45,7 +45,11 @@ typedef struct asd_ops asd_ops; /* opaque: the device, and an error word on it *
 
 typedef enum { ASD_TYPE_F32 = 0, ASD_TYPE_F16 = 1, ASD_TYPE_BF16 = 2 } asd_type;
 
-/* SILU: g / (1 + exp(-g)).  GELU: g Phi(g) with the normal distribution function (erf form). */
+/*
+ * SILU: g / (1 + exp(-g)).  GELU: g Phi(g) with the normal distribution function (not the tanh form).  Both are computed in 32 bits
+ * with the approximate exponential and reciprocal, for every type: off by at most (4 + |g|) 2^-23 and (8 + g^2) 2^-23 of their
+ * value, as long as that is above 2^-119 (below, they may be 0).
+ */
 typedef enum { ASD_ACT_NONE = 0, ASD_ACT_SILU = 1, ASD_ACT_GELU = 2 } asd_act;
 
 asd_status asd_ops_create(asd_ops** out);

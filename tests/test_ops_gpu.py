@@ -566,3 +566,41 @@ def test_refusals_of_the_c_entry_points(ops):
     a.workspace, a.workspace_bytes = space.data_ptr() + 128, need.value
     assert lib.asd_gated_mlp_forward(h, C.byref(a), st) == 1
     ops.check()
+
+
+# ---- gates far on the negative side ---------------------------------------------------------------------
+
+def gate64(g, act):
+    """act(g), and what of it 32 bits may lose: the header's bounds of the normal distribution function and the sigmoid, and a product."""
+    if act == "silu":
+        return g * torch.sigmoid(g), (4 + g.abs() + 1) * 2.0 ** -23
+    return g * 0.5 * torch.erfc(-g / math.sqrt(2)), (8 + g * g + 1) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width", [(5, 64), (7, 100), (4, 1000), (1300, 264), (3, 1003), (2, 16390), (2, 17000)])
+def test_quantize_of_gates_that_are_all_negative(ops, rows, width, kind, act):
+    """A row whose largest value is itself far down the gate's tail: it is held to a relative error, not to one of 1."""
+    g = torch.rand((rows, width), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda") * -2 - 4
+    x = torch.cat([g, rand((rows, width), 2)], 1).to(TYPES[kind])
+    q, scale = ops.quantize_i8(x, act=act)
+    g, u = x[:, :width].to(F64), x[:, width:].to(F64)
+    a, slack = gate64(g, act)
+    check_q8(q, scale, a * u, slack=2 * (float(slack.max()) + 4 * 2.0 ** -24))
+
+
+@pytest.mark.parametrize("rows", [4, 64, 2048])
+def test_gated_mlp_of_gates_that_are_all_negative(ops, rows):
+    """Rows of the identity through the weights, so that g and u are the weights' own values and y is h: rounded once to h, and
+    exact from there on."""
+    d, t = 64, torch.float16
+    g = (torch.rand((d, d), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda") * -1 - 4).to(t)
+    u = (torch.rand((d, d), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda") * 4096 + 4096).to(t)
+    one = torch.eye(d, device="cuda", dtype=t)
+    x = one.repeat((rows + d - 1) // d, 1)[:rows]
+    for act in ("silu", "gelu"):
+        y = ops.gated_mlp(x, torch.cat([g, u]), one, act=act)
+        a, slack = gate64(x.to(F64) @ g.to(F64).T, act)
+        want = a * (x.to(F64) @ u.to(F64).T)
+        within(y, want, want.abs() * (U[t] + slack + 2.0 ** -22), act)
