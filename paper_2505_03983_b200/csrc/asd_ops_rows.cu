@@ -780,9 +780,9 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
       sq += buf[side][0][i];
       dot += buf[side][1][i];
     }
-    // dx = rho (dy w - s rho c) + ds with c = mean(dy w z) = rho dot / width
+    // dx = rho dy w - z (rho c) + ds with c = mean(dy w z) = rho dot / width; s times rho first: rho^2 c may leave the range of 32 bits
     const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
-    const float k = -(rho * dot / (float)a.width) * rho * rho;
+    const float k = -(rho * dot / (float)a.width) * rho;
     const float2 rho2 = make_float2(rho, rho), k2 = make_float2(k, k);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -795,8 +795,9 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_kernel(const NormGradArgs a)
         float d[2 * NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          acc[v][i] = fma2(g[v][i], mul2(f[v][i], rho2), acc[v][i]);
-          const float2 x = fma2(f[v][i], k2, fma2(mul2(g[v][i], w[v][i]), rho2, e[i]));
+          const float2 z = mul2(f[v][i], rho2);
+          acc[v][i] = fma2(g[v][i], z, acc[v][i]);
+          const float2 x = fma2(z, k2, fma2(mul2(g[v][i], w[v][i]), rho2, e[i]));
           d[2 * i] = x.x;
           d[2 * i + 1] = x.y;
         }
@@ -1064,11 +1065,12 @@ __global__ void __launch_bounds__(kNarrowBlock) narrow_grad_kernel(const NormGra
       sq = group_sum<L>(sq);
       dot = group_sum<L>(dot);
       const float rho = 1.f / sqrtf(sq / (float)a.width + a.eps);
-      const float k = -(rho * dot / (float)a.width) * rho * rho;
+      const float k = -(rho * dot / (float)a.width) * rho;
 #pragma unroll
       for (int i = 0; i < kNarrow; ++i) {
-        if (live) acc[i] = fmaf(g[u][i], f[u][i] * rho, acc[i]);
-        e[u][i] = fmaf(f[u][i], k, fmaf(g[u][i] * w[i], rho, e[u][i]));
+        const float z = f[u][i] * rho;
+        if (live) acc[i] = fmaf(g[u][i], z, acc[i]);
+        e[u][i] = fmaf(z, k, fmaf(g[u][i] * w[i], rho, e[u][i]));
       }
       if (live) narrow_store<VEC, L, T>(reinterpret_cast<T*>(a.dx) + row * a.ld_dx, a.width, t, e[u]);
     }

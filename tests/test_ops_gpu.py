@@ -604,3 +604,21 @@ def test_gated_mlp_of_gates_that_are_all_negative(ops, rows):
         a, slack = gate64(x.to(F64) @ g.to(F64).T, act)
         want = a * (x.to(F64) @ u.to(F64).T)
         within(y, want, want.abs() * (U[t] + slack + 2.0 ** -22), act)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width", [(5, 64), (7, 33), (1300, 200), (4, 1000), (3, 1001), (2, 4096), (2, 5001), (2, 9000)])
+def test_norm_gradient_of_very_small_rows(ops, rows, width, kind):
+    """Rows whose rho is 10^19 with eps = 0: no factor of the gradient leaves the range of 32 bits while the gradient does not."""
+    t = TYPES[kind]
+    sign = torch.where(rand((rows, width), 1) < 0, -1.0, 1.0)
+    s = ((1 + torch.rand((rows, width), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")) * 1e-19 * sign).to(t)
+    dy, w = (100 * (sign + rand((rows, width), 3))).to(t), (1 + 0.1 * rand((width,), 4)).to(t)
+    dx, dw = ops.add_rmsnorm_backward(dy, s, w, eps=0.0)
+    _, f, rho, _ = norm64(s, None, w, 0.0)
+    z, dz = f * rho, dy.to(F64) * w.to(F64)
+    want = rho * (dz - z * (dz * z).mean(-1, keepdim=True))
+    big = rho * (dz.abs() + z.abs() * (dz * z).abs().mean(-1, keepdim=True))
+    within(dx, want, want.abs() * U[t] + big * 1e-5, "dx")
+    terms = dy.to(F64) * z
+    within(dw, terms.sum(0), terms.sum(0).abs() * U[t] + terms.abs().sum(0) * (GAMMA(rows) + 1e-5), "dw")
