@@ -1,6 +1,8 @@
-"""Build the CUDA library in-tree: nvcc, sm_100a only, one shared object next to this file."""
+"""Build the CUDA library in-tree: nvcc, sm_100a only, one shared object next to this file; and, where torch is installed, the
+operators' binding for its tensors beside it.  A caller of the C entry points needs the first alone."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -17,12 +19,17 @@ TORCH_LIB = os.path.join(HERE, "_asd_torch.so")  # the operators for torch tenso
 
 
 def _build_torch_binding(force: bool) -> None:
-    """csrc/asd_torch.cpp against this environment's torch, next to the library it calls."""
-    src = os.path.join(HERE, "csrc", "asd_torch.cpp")
-    if not force and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) >= _newest([src, os.path.join(ROOT, "include", "asd_ops.h")]):
+    """csrc/asd_torch.cpp against this environment's torch, next to the library it calls; without torch there is none."""
+    if importlib.util.find_spec("torch") is None:
         return
     import sysconfig
     import torch
+    src = os.path.join(HERE, "csrc", "asd_torch.cpp")
+    # what it was built for: the interfaces of torch and Python change from version to version
+    built, this = os.path.splitext(TORCH_LIB)[0] + ".built", f"torch {torch.__version__}, Python {sysconfig.get_python_version()}\n"
+    if not force and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) >= _newest([src, os.path.join(ROOT, "include", "asd_ops.h")]) and \
+            os.path.exists(built) and open(built).read() == this:
+        return
     from torch.utils import cpp_extension as ext
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w",
@@ -33,7 +40,9 @@ def _build_torch_binding(force: bool) -> None:
             "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch", "-ltorch_python"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("g++ failed on " + src + ":\n" + res.stdout + res.stderr)
+        raise RuntimeError("the C library is built; g++ failed on its torch binding, " + src + ":\n" + res.stdout + res.stderr)
+    with open(built, "w") as f:
+        f.write(this)
 
 
 def _newest(paths):
