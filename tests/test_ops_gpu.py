@@ -622,3 +622,30 @@ def test_norm_gradient_of_very_small_rows(ops, rows, width, kind):
     within(dx, want, want.abs() * U[t] + big * 1e-5, "dx")
     terms = dy.to(F64) * z
     within(dw, terms.sum(0), terms.sum(0).abs() * U[t] + terms.abs().sum(0) * (GAMMA(rows) + 1e-5), "dw")
+
+
+def test_first_call_of_a_thread(ops):
+    """A thread on which nothing of CUDA has run yet: the first call there is the operator's."""
+    import threading
+    for rows in (4, 40, 300, 2048):
+        x, dy, wi, wo = mlp_data(rows, 256, 512, torch.bfloat16)
+        q, scale = ops.quantize_i8(x)
+        w = ops.quantize_i8(wi)
+        _, saved = ops.gated_mlp_forward(x, wi, wo)
+        for f in (lambda: (ops.gated_mlp(x, wi, wo),), lambda: ops.gated_mlp_backward(dy, x, wi, wo, saved), lambda: (ops.matmul_i8(q, scale, *w),),
+                  lambda: ops.quantize_i8(x, act="silu"), lambda: ops.add_rmsnorm(x, None, residual=dy)):
+            want, got = f(), []
+            del want  # its memory, so that none is asked for on the thread
+            torch.cuda.synchronize()
+
+            def work():
+                try:
+                    got.append(f())
+                except BaseException as e:  # noqa: B902
+                    got.append(e)
+
+            thread = threading.Thread(target=work)
+            thread.start()
+            thread.join()
+            assert not isinstance(got[0], BaseException), (rows, got[0])
+            assert all(torch.equal(a, b) for a, b in zip(got[0], f()))
