@@ -649,3 +649,132 @@ def test_first_call_of_a_thread(ops):
             thread.join()
             assert not isinstance(got[0], BaseException), (rows, got[0])
             assert all(torch.equal(a, b) for a, b in zip(got[0], f()))
+
+
+# ---- exact sums, several callers, and the error word ------------------------------------------------------
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,width,hidden", [(1, 1030, 500), (8, 1030, 500), (40, 1030, 500), (300, 1030, 500), (2050, 1030, 516), (5000, 264, 300),
+                                               (9000, 100, 333)])
+def test_gated_mlp_is_exact(ops, rows, width, hidden, kind, act):
+    """Whole numbers (w_out: 64ths) whose sums stay below 2^24 units, with every gate at 32 or more, where act(g) = g and act'(g) = 1
+    in 32 bits: then only the roundings to 16 bits are left, and a product that is lost, doubled or out of place shows."""
+    t = TYPES[kind]
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def whole(low, high, *shape):
+        return torch.randint(low, high + 1, shape, generator=gen, device="cuda").to(F64)
+
+    x, dy, wu, wo = whole(1, 2, rows, width), whole(-1, 1, rows, width), whole(-1, 1, hidden, width), whole(-1, 1, width, hidden) / 64
+    wg = torch.zeros((hidden, width), dtype=F64, device="cuda")
+    wg.scatter_(1, torch.rand((hidden, width), generator=gen, device="cuda").argsort(1)[:, :40], 1.0)
+
+    def round16(v):
+        return v.to(torch.float32).to(t).to(F64)
+
+    g, u = x @ wg.T, x @ wu.T
+    h, dh = round16(g * u), dy @ wo
+    d = torch.cat([round16(dh * u), round16(dh * g)], 1)
+    w_in = torch.cat([wg, wu])
+    sums = {"y": (h, wo.T), "dx": (d, w_in), "dw_in": (d.T, x), "dw_out": (dy.T, h)}
+    for name, (a, b) in sums.items():
+        units = 1 if name == "dw_out" else 64
+        assert float((a.abs() @ b.abs()).max()) * units < 2 ** 24, name
+    assert float(g.min()) >= 32 and float(u.abs().max()) < 2 ** 15
+    v = [m.to(t) for m in (x, w_in, wo)]
+    y, saved = ops.gated_mlp_forward(*v, act=act)
+    got = dict(zip(("dx", "dw_in", "dw_out"), ops.gated_mlp_backward(dy.to(t), *v, saved, act=act)), y=y)
+    assert torch.equal(ops.gated_mlp(*v, act=act), y)
+    for name, (a, b) in sums.items():
+        assert torch.equal(got[name].to(F64), round16(a @ b)), name
+
+
+def test_matmul_i8_is_exact_at_the_extremes(ops):
+    """-128 times -128, where it is the longest sum below 2^24, beside other values by row, column and place in the sum."""
+    one = torch.ones
+    for rows, k, out in ((1, 1023, 300), (8, 1023, 300), (40, 1023, 300), (300, 1023, 300), (5000, 1023, 300)):
+        a, b = (torch.full((n, k), -128, dtype=torch.int8, device="cuda") for n in (rows, out))
+        r, c, i = (torch.arange(n, device="cuda") for n in (rows, out, k))
+        a[r, (7 * r + 3) % k] = (r % 100).to(torch.int8)
+        b[c, (11 * c + 5) % k] = (c % 90 - 127).to(torch.int8)
+        b[:, i % 97 == 13] = 127
+        want = a.to(F64) @ b.to(F64).T
+        assert float((a.to(F64).abs() @ b.to(F64).abs().T).max()) < 2 ** 24
+        y = ops.matmul_i8(a, one(rows, device="cuda"), b, one(out, device="cuda"), dtype=torch.float32)
+        assert torch.equal(y.to(F64), want)
+
+
+def step_of(ops, rows, seed):
+    t = torch.bfloat16
+    x, dy, wi, wo = mlp_data(rows, 264, 520, t)
+    x, w = rand((rows, 264), seed, t), rand((264,), 9, t)
+
+    def step():
+        n, s = ops.add_rmsnorm(x, w, residual=dy)
+        y, saved = ops.gated_mlp_forward(n, wi, wo)
+        g = ops.gated_mlp_backward(dy, n, wi, wo, saved)
+        q, sc, _ = ops.add_rmsnorm_i8(x, w, residual=dy)
+        i8 = ops.matmul_i8(q, sc, *ops.quantize_i8(wi))
+        return [y, *g, *ops.add_rmsnorm_backward(g[0], s, w, ds=dy), i8, *ops.quantize_i8(i8, act="silu")]
+
+    return step
+
+
+def test_several_streams_and_threads_at_once(ops):
+    """One handle, four streams with work in flight together, from one thread and from four: the bits of each alone."""
+    import threading
+    steps = [step_of(ops, rows, 20 + i) for i, rows in enumerate((4, 60, 400, 1500))]
+    alone = [s() for s in steps]
+    streams = [torch.cuda.Stream() for _ in steps]
+    torch.cuda.synchronize()
+    got = [[] for _ in steps]
+    for _ in range(10):
+        for i, s in enumerate(steps):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(s())
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(streams[i]):
+                for _ in range(10):
+                    got[i].append(steps[i]())
+                streams[i].synchronize()
+        except BaseException as e:  # noqa: B902
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(steps))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    for i, runs in enumerate(got):
+        assert len(runs) == 20
+        for run in runs:
+            assert all(torch.equal(a, b) for a, b in zip(run, alone[i])), i
+    ops.check()
+
+
+ASD_ERR_TIMEOUT = 6
+
+
+def test_check_reports_a_wait_that_ran_out(ops):
+    """The word that a kernel sets when it gives up a wait, set here by the host: reported once, by its own status, and no obstacle
+    to what comes after it."""
+    import ctypes as C
+    from paper_2505_03983_b200 import AsdError, AsdOps
+    with AsdOps() as other:
+        word = C.c_void_p.from_address(other._handle + 8).value  # behind the device's number and that of its SMs
+        x = rand((4, 64), 1)
+        want = other.quantize_i8(x)
+        torch.cuda.synchronize()
+        assert C.CDLL("libcuda.so.1").cuMemsetD32_v2(C.c_uint64(word), C.c_uint32(ASD_ERR_TIMEOUT), C.c_size_t(1)) == 0
+        with pytest.raises(AsdError) as e:
+            other.check()
+        assert e.value.status == ASD_ERR_TIMEOUT and "limit" in str(e.value)
+        other.check()
+        ops.check()
+        assert all(torch.equal(a, b) for a, b in zip(other.quantize_i8(x), want))
