@@ -91,8 +91,8 @@ asd_status asd_add_rmsnorm(asd_ops* ops, const asd_rmsnorm_args* args, void* cud
  * Gradients of the form without scale: with z = s rho, rho = 1 / sqrt(mean(s^2) + eps),
  *   dx = rho (dy w - z mean(dy w z)) + ds        (the gradient of x and of the residual alike)
  *   dw = sum over rows of dy z                   (w_type)
- * ds, the gradient that reaches s itself, may be NULL (0).  dw may be NULL (not computed); weight NULL means 1,
- * with dw in F32 unless w_type says otherwise.
+ * ds, the gradient that reaches s itself, may be NULL (0).  dx and dw may each be NULL (not computed); weight NULL
+ * means 1, with dw in F32 unless w_type says otherwise.
  */
 typedef struct {
   int32_t rows, width;

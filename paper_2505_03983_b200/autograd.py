@@ -49,9 +49,10 @@ class _AddRmsnorm(torch.autograd.Function):
     def backward(ctx, dy, ds):
         s, weight = ctx.saved_tensors
         need_dw = weight is not None and ctx.needs_input_grad[1]
+        need_dx = ctx.needs_input_grad[0] or ctx.needs_input_grad[2]
         if dy is None:  # only s was used
             return ds, torch.zeros_like(weight) if need_dw else None, ds if ctx.has_residual else None, None
-        dx, dw = default_ops().add_rmsnorm_backward(dy, s, weight, ds=ds, eps=ctx.eps, need_dweight=need_dw)
+        dx, dw = default_ops().add_rmsnorm_backward(dy, s, weight, ds=ds if need_dx else None, eps=ctx.eps, need_dweight=need_dw, need_dx=need_dx)
         dx, dw = _first_only((dx, dw), s, weight, dy, ds)
         return dx, dw, dx if ctx.has_residual else None, None
 

@@ -251,7 +251,7 @@ asd_status check_norm_backward(const asd_ops* o, const asd_rmsnorm_backward_args
   CHECK(check_mat("dy", a->dy, a->ld_dy, a->rows, a->width, es));
   CHECK(check_mat("s", a->s, a->ld_s, a->rows, a->width, es));
   if (a->ds) CHECK(check_mat("ds", a->ds, a->ld_ds, a->rows, a->width, es));
-  CHECK(check_mat("dx", a->dx, a->ld_dx, a->rows, a->width, es));
+  if (a->dx) CHECK(check_mat("dx", a->dx, a->ld_dx, a->rows, a->width, es));
   return ASD_OK;
 }
 
@@ -375,6 +375,7 @@ asd_status asd_add_rmsnorm_backward(asd_ops* o, const asd_rmsnorm_backward_args*
   CHECK(check_device(o));
   cudaStream_t st = (cudaStream_t)stream;
   if (a->rows == 0) return a->dw ? zero(a->dw, a->width, 1, a->width, ops_type_size(a->w_type), st) : ASD_OK;
+  if (!a->dx && !a->dw) return ASD_OK;
   launch_rmsnorm_backward(o, a, st);
   return ops_launched("add_rmsnorm_backward");
 }

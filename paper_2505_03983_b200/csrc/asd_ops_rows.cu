@@ -654,7 +654,7 @@ struct NormGradArgs {
   int pitch;    // of a staged row
   float eps;
   const void *dy, *s, *ds, *w;
-  void* dx;
+  void* dx;     // or NULL
   float* part;  // [blocks, width] sums of dy z over a block's rows, or NULL
   float* rho;   // LONG: [rows]
   int64_t ld_dy, ld_s, ld_ds, ld_dx;
@@ -1072,7 +1072,7 @@ __global__ void __launch_bounds__(kNarrowBlock) narrow_grad_kernel(const NormGra
         if (live) acc[i] = fmaf(g[u][i], z, acc[i]);
         e[u][i] = fmaf(z, k, fmaf(g[u][i] * w[i], rho, e[u][i]));
       }
-      if (live) narrow_store<VEC, L, T>(reinterpret_cast<T*>(a.dx) + row * a.ld_dx, a.width, t, e[u]);
+      if (live && a.dx) narrow_store<VEC, L, T>(reinterpret_cast<T*>(a.dx) + row * a.ld_dx, a.width, t, e[u]);
     }
   }
   if (!a.part) return;

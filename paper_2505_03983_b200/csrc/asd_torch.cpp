@@ -150,7 +150,7 @@ py::tuple add_rmsnorm(int64_t ops, int device, const Tensor& x, const OptTensor&
 }
 
 py::tuple add_rmsnorm_backward(int64_t ops, int device, const Tensor& dy, const Tensor& s, const OptTensor& weight, const OptTensor& ds, double eps,
-                               bool need_dw) {
+                               bool need_dw, bool need_dx) {
   const Call c{(asd_ops*)ops, device};
   asd_rmsnorm_backward_args a{};
   a.type = a.w_type = type_of(s, "s");
@@ -164,20 +164,23 @@ py::tuple add_rmsnorm_backward(int64_t ops, int device, const Tensor& dy, const 
     same_shape(*ds, "ds", s);
     a.ds = d.p(), a.ld_ds = d.ld;
   }
-  Tensor w, dw, dx = c.empty(s.sizes(), s.scalar_type());
+  Tensor w, dw, dx;
   if (weight) {
     w = vector_of(c, *weight, "weight", m.w, std::nullopt);
     a.w_type = type_of(w, "weight");
     a.weight = w.data_ptr();
   }
-  a.dx = dx.data_ptr(), a.ld_dx = m.w;
+  if (need_dx) {
+    dx = c.empty(s.sizes(), s.scalar_type());
+    a.dx = dx.data_ptr(), a.ld_dx = m.w;
+  }
   if (need_dw) {
     dw = c.empty({m.w}, scalar_of(a.w_type));
     a.dw = dw.data_ptr();
   }
   const Tensor space = workspace(c, &a, asd_add_rmsnorm_backward_workspace);
   check(asd_add_rmsnorm_backward(c.ops, &a, c.stream()));
-  return py::make_tuple(std::move(dx), need_dw ? py::cast(std::move(dw)) : py::none());
+  return py::make_tuple(need_dx ? py::cast(std::move(dx)) : py::none(), need_dw ? py::cast(std::move(dw)) : py::none());
 }
 
 py::tuple quantize_i8(int64_t ops, int device, const Tensor& x, int act) {

@@ -157,10 +157,10 @@ class AsdOps:
         """(q, scale, s): as add_rmsnorm, with y ~ q * scale[..., None] in int8 and a float32 scale per row."""
         return self._ext.add_rmsnorm(self._handle, self.device, x, weight, residual, eps, True)
 
-    def add_rmsnorm_backward(self, dy, s, weight, ds=None, eps=1e-6, need_dweight=True):
+    def add_rmsnorm_backward(self, dy, s, weight, ds=None, eps=1e-6, need_dweight=True, need_dx=True):
         """(dx, dweight) of add_rmsnorm from the gradients dy of y and ds of s (None: 0); dx is the gradient of x and of
-        the residual alike, dweight has weight's type (s's without a weight), or is None if it is not needed."""
-        return self._ext.add_rmsnorm_backward(self._handle, self.device, dy, s, weight, ds, eps, need_dweight)
+        the residual alike, dweight has weight's type (s's without a weight); one that is not needed is None."""
+        return self._ext.add_rmsnorm_backward(self._handle, self.device, dy, s, weight, ds, eps, need_dweight, need_dx)
 
     # -- 8 bits ----------------------------------------------------------------------------
     def quantize_i8(self, x, act: Optional[str] = None):

@@ -20,12 +20,13 @@ class Stand:
         return (y if weight is None else y * weight), s
 
     @torch.no_grad()
-    def add_rmsnorm_backward(self, dy, s, weight, ds=None, eps=1e-6, need_dweight=True):
+    def add_rmsnorm_backward(self, dy, s, weight, ds=None, eps=1e-6, need_dweight=True, need_dx=True):
+        self.needed_dx = need_dx
         self.calls.append(("add_rmsnorm_backward", ds is not None, need_dweight))
         rho = torch.rsqrt(s.square().mean(-1, keepdim=True) + eps)
         z, dz = s * rho, dy if weight is None else dy * weight
         dx = rho * (dz - z * (dz * z).mean(-1, keepdim=True))
-        return (dx if ds is None else dx + ds), ((dy * z).sum(0) if need_dweight else None)
+        return (None if not need_dx else dx if ds is None else dx + ds), ((dy * z).sum(0) if need_dweight else None)
 
     @torch.no_grad()
     def gated_mlp(self, x, w_in, w_out, act="silu"):
@@ -142,3 +143,17 @@ def test_outputs_that_are_not_used_bring_no_zeros(stand):
     y = s * torch.rsqrt(s.square().mean(-1, keepdim=True) + 1e-6) * w
     for a, b in zip(got, torch.autograd.grad((y.square().sum() + s.pow(3).sum()), (x, w, r))):
         assert torch.allclose(a, b)
+
+
+def test_a_gradient_that_nothing_needs_is_not_computed(stand):
+    """The first norm of a network: its inputs are data, its weight a parameter."""
+    x, r, w = make(5, 8), make(5, 8, seed=1), make(8, seed=2).requires_grad_()
+    for residual in (None, r):
+        y, s = autograd.add_rmsnorm(x, w, residual)
+        y.square().sum().backward()
+        assert stand.calls[-1] == ("add_rmsnorm_backward", False, True) and not stand.needed_dx
+    for leaf in (x, r):
+        leaf.requires_grad_()
+        autograd.add_rmsnorm(x, w, r)[0].sum().backward()
+        assert stand.needed_dx and leaf.grad is not None
+        leaf.requires_grad_(False)

@@ -778,3 +778,16 @@ def test_check_reports_a_wait_that_ran_out(ops):
         other.check()
         ops.check()
         assert all(torch.equal(a, b) for a, b in zip(other.quantize_i8(x), want))
+
+
+@pytest.mark.parametrize("rows,width", [(6, 64), (700, 33), (6, 1000), (1500, 1001), (6, 5000), (6, 9000), (6, 17003)])
+def test_norm_gradient_parts(ops, rows, width):
+    """Each gradient on its own has the bits that it has beside the other; neither is a valid call."""
+    t = torch.bfloat16
+    s, dy, ds, w = rand((rows, width), 1, t), rand((rows, width), 2, t), rand((rows, width), 4, t), rand((width,), 3, t)
+    dx, dw = ops.add_rmsnorm_backward(dy, s, w, ds=ds)
+    none, alone = ops.add_rmsnorm_backward(dy, s, w, need_dx=False)
+    assert none is None and torch.equal(alone, dw)
+    alone, none = ops.add_rmsnorm_backward(dy, s, w, ds=ds, need_dweight=False)
+    assert none is None and torch.equal(alone, dx)
+    assert ops.add_rmsnorm_backward(dy, s, w, need_dx=False, need_dweight=False) == (None, None)
