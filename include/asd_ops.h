@@ -15,8 +15,9 @@
  *  - Pointers are device memory of the device that was current in asd_ops_create, which must be current in the
  *    call; matrices are row-major with contiguous rows, ld_* is the distance of two rows in ELEMENTS
  *    (>= the row's length).  Any length, distance and element-aligned address is accepted: operands of the matrix
- *    products whose address or distance is not a multiple of 16 bytes are copied to the workspace first, and
- *    rows of the other operators are then read element by element.
+ *    products whose address or distance is not a multiple of 16 bytes are copied to the workspace first; such rows of
+ *    the other operators come through shared memory in aligned pieces (up to 256 elements, and over 16384 or, in
+ *    the norm's gradient, 8192: element by element).
  *  - Work is enqueued on the stream given in the call (a cudaStream_t as void*; NULL = the default stream) and the
  *    call returns.  No call synchronises, allocates or keeps anything of its inputs, so calls may be captured in
  *    a CUDA graph, and one handle may serve several streams and threads.
@@ -25,7 +26,7 @@
  *  - No output may overlap an input or another output, except that asd_add_rmsnorm's sum may be its x or its
  *    residual, and asd_add_rmsnorm_backward's dx its dy or ds, with the same row distance.
  *  - Zero rows is a valid call that does nothing (gradients of weights are then set to zero).
- *  - Sums, statistics and the activation are in 32 bits.  Results do not depend on the order in which blocks of a
+ *  - Sums, statistics and the activation are in 32 bits (the norm of a row whose sum of squares is beyond them is 0).  Results do not depend on the order in which blocks of a
  *    kernel run: the same inputs give the same bits.
  *  - A call that returns an error has enqueued nothing, except for CUDA: a launch failed after others may have been
  *    enqueued, and the outputs are undefined.
@@ -147,7 +148,8 @@ asd_status asd_matmul_i8(asd_ops* ops, const asd_matmul_i8_args* args, void* cud
  * first, w_out [width, hidden], y [rows, width]; F16 or BF16 throughout (UNSUPPORTED otherwise), sums in fp32, h
  * rounded to the type, act SILU or GELU.
  * saved != NULL: what asd_gated_mlp_backward needs is kept there (asd_gated_mlp_saved gives its bytes; address
- * 256-byte aligned, layout private to the library).
+ * 256-byte aligned, layout private to the library): h, and the gate's two factors u act'(g) and act(g) in the upper 24
+ * of their 32 bits, truncated (off by less than 2^-15 of themselves, towards zero).
  */
 typedef struct {
   int32_t rows, width, hidden;

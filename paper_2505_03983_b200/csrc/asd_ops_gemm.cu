@@ -758,8 +758,9 @@ asd_status ops_gemm_list(const asd_ops* o, const OpsGemm* list, int count, cudaS
 // The gradient of a narrow weight is a few tiles with a sum over all rows, which a few pairs would walk along while the
 // others are idle.  Up to a sixth of the pairs' number of tiles are therefore cut into as many slices as there are pairs, of
 // 16 k-blocks at least.  All gradients of the gated MLP, with slices against without: 32768 x 256 x 512 (2 tiles) 96 us
-// against 228, 131072 x 256 x 1024 (4) 565 against 1115, 32768 x 512 x 1280 (10) 273 against 356, 4096 x 512 x 1536 (12) 65
-// against 62.  Beyond that the input's gradient in the same launch keeps the pairs busy and the partial sums only cost: 4096 x
+// against 228, 131072 x 256 x 1024 (4) 565 against 1115, 32768 x 512 x 1280 (10) 273 against 356; with 12 tiles the
+// two meet at some 4096 rows (512 x 1536: 2048 rows 51 against 49, 4096 65 against 63, 8192 97 against 111, 32768 332 against 447).
+// Beyond that the input's gradient in the same launch keeps the pairs busy and the partial sums only cost: 4096 x
 // 512 x 2048 (16) 80 against 70, 8192 x 768 x 2048 (24) 184 against 167.  It goes by the sizes of the one product alone, so
 // that a gradient has the same bits whichever others are asked for.
 int sum_slices(const asd_ops* o, int64_t m, int64_t n, int64_t k) {

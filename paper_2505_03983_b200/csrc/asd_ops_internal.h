@@ -26,8 +26,11 @@ void ops_note_launch(cudaError_t e);        // what a launch returned, kept unti
 asd_status ops_launched(const char* what);  // OK, or CUDA with the first error of this thread's launches since the last call
 int ops_type_size(int type);                // bytes of an asd_type, 0 if it is none
 
-// Launch with programmatic stream serialization: the kernel may start while its predecessor in the stream ends; every
-// kernel of this library waits for it (griddepcontrol.wait) before it touches global memory.
+// Launch with programmatic stream serialization: the kernel may start while its predecessor in the stream ends.  Every kernel of the
+// operators waits for it (griddepcontrol.wait) before it touches global memory, and lets its own successor start
+// (griddepcontrol.launch_dependents) only after that wait.  The split and the stream kernel with `early` read their weights
+// before the wait: that the kernel before them was let in only after its own wait is what makes it safe, for then everything
+// further back has ended, and the kernel before them is of the same call and does not write the weights.
 template <typename... P, typename... A>
 inline void ops_launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, int cluster, A... args) {
   cudaLaunchConfig_t cfg = {};

@@ -9,8 +9,10 @@
 // 16-byte pieces that hold them, one row ahead, and are read from there element by element, neighbouring threads on neighbouring
 // elements (read so from memory, 6001 rows of 2 x 2477 bf16 took 127 us to quantise).
 //
-// Measured (of 6.55 TB/s): norm 8192 x 4096 bf16 43 us = 6.2 TB/s, to int8 32768 x 1024 42.6 us = 5.5 TB/s, gradient 8192 x 4096 52 us =
-// 5.2 TB/s, gate to int8 8192 x 8192 56.6 us = 5.9 TB/s.  One row of 4096 takes 4 us, a kernel's start and end.
+// Measured (of 6.55 TB/s): norm 8192 x 4096 bf16 43 us = 6.2 TB/s, to int8 32768 x 1024 42.6 us = 5.5 TB/s, gradient 8192 x 4096 44 us =
+// 6.1 TB/s, gate to int8 8192 x 8192 56.6 us = 5.9 TB/s with SiLU and 77 with GELU, whose instructions fill 79 % of
+// the issue slots.  float32: norm 8192 x 4096 84 us = 6.4 TB/s, gradient 142 (3.8), rows to int8 without the gate 24, gate 8192 x 8192 90
+// (6.7) and 93.  Rows of 16384, 4096 of them in bf16: norm 97, gradient 193 for dx, 118 for dw.  One row of 4096 takes 4 us, a kernel's start and end.
 #include <type_traits>
 
 #include "asd_ops_act.cuh"

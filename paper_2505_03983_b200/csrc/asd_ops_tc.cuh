@@ -1,6 +1,6 @@
 // Device-side pieces shared by the operators' tensor-core kernels: shared-memory descriptors of both operand orders, the
 // MMA of each operand kind, the gated activation with its gradient, and the 24-bit form in which a training step keeps
-// the two projections.  Everything here has internal linkage.
+// the gate's two factors.  Everything here has internal linkage.
 #pragma once
 
 #include "asd_ops_act.cuh"
@@ -108,7 +108,8 @@ __device__ __forceinline__ void gated(float (&g)[N], float (&u)[N], float (&h)[N
 // What a training step keeps of the gate.  h = act(g) u has the derivatives act(g) in u and u act'(g) in g, and it is these
 // two factors that are kept: the backward pass then multiplies dh by them, without an exponential.  Rounding them to bf16
 // would make the gradients' error half as large again as the roundings of dg, du and the result make it; fp32 would double
-// the traffic.  Kept are the upper 24 bits of the fp32 value (truncated: sign, exponent and 15 bits, an error below 2^-15),
+// the traffic.  Kept are the upper 24 bits of the fp32 value (truncated: sign, exponent and 15 bits, an error below 2^-15, always towards zero: a
+// 128th of the rounding of dg and du to bf16, a 16th of that to fp16; rounding them would take an addition and a guard for NaN each),
 // the upper 16 and the next 8 in separate vectors.  The order is that of the accumulator tiles, where a thread holds 32
 // neighbouring columns of a row: a block is 32 rows x 32 columns of u act'(g), then of act(g), each as 4 + 2 vectors of 16
 // bytes for every row, vector by vector, so that a warp's stores and loads are whole 512-byte runs.
