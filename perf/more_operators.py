@@ -193,9 +193,6 @@ def prepare(case, seed):
             s["v"] = flat(torch.clamp(torch.round(180 + 30 * normal(total)), 1, 255).to(torch.uint8))
             s["scales"] = torch.stack([size.flatten(), 2 * size.flatten()], dim=1).contiguous()
         s["step"] = torch.tensor([9 + int(seed) % 50, 0], device="cuda")  # the steps taken; the second word is the library's
-        s["lists"] = {k: _split(s[k], case) for k in ("p", "g", "m", "v", "master") if s[k] is not None}  # a network's tensors, one by one
-        if case["bits"] == 8:
-            s["lists"]["scales"] = list(s["scales"].split([_padded(n) // BLOCK for n in sizes]))
     return s
 
 
@@ -348,9 +345,13 @@ def _library(s):
         dx, dr, dw, dw_post, dgate = ops.block_rmsnorm_backward(dy, x, total, s["w"], ds=ds, **how)
         out |= {"dr": dr.view(s["x"].shape), "dw": dw, "dgate": dgate.view(s["gate"].shape), "dx": dx.view(s["x"].shape)}
         return {**out, "dw_post": dw_post} if case["post"] else out
-    lists = s["lists"]
+    lists = {k: _split(s[k], case) for k in ("p", "g", "m", "v")}
+    masters = _split(s["master"], case) if case["master"] else None
+    scales = None
+    if case["bits"] == 8:
+        scales = [v.view(-1, 2) for v in s["scales"].flatten().split([_padded(n) // BLOCK * 2 for n in _sizes(case)])]
     ops.adamw(lists["p"], lists["g"], lists["m"], lists["v"], s["step"], lr=LR, betas=(BETA1, BETA2), eps=ADAM_EPS, weight_decay=DECAY,
-              masters=lists.get("master"), scales=lists.get("scales"))
+              masters=masters, scales=scales)
     out = {"p": s["p"], "master": s["master"]} if case["master"] else {"p": s["p"]}
     if case["bits"] == 32:
         return {**out, "m": s["m"], "v": s["v"]}
