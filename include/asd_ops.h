@@ -313,12 +313,17 @@ asd_status asd_block_rmsnorm_backward(asd_ops* ops, const asd_block_rmsnorm_back
  *   m = M (q / 127) |q / 127|,   M = max |m|,           q rounded to nearest
  *   v = (R (q / 255)^2)^2,       R = max sqrt(v),       q rounded to nearest, and 1 at least where v > 0
  * a scale below 2^-100 is 0, with q = 0; a NaN or an infinity among a block's moments makes its scale NaN and its q 0.  The
- * step itself is taken with the moments before they are rounded.
+ * step itself is taken with the moments before they are rounded.  Rounded to the nearest, a q follows no decay that is smaller than
+ * half a step, (1 - beta1) q < 1 or (1 - beta2) q < 2: with a beta2 of 0.999 sqrt(v) grows beside its true value over the steps, by
+ * 4 % in 1000 and a third in 10000 where a block's gradients are of one size.
+ * bits 8 | ASD_ADAMW_UNBIASED: the same codes, with q rounded up with the probability of its fraction, or down, so that its mean follows.
+ * Whether it is comes from the number of the step and the element's place in its tensor: the same in every run.
  * step: two words on the device, the number of steps taken and one that the library uses (0 at first, and between calls); the
  * call moves the first on by one, so that a captured call may be replayed.  lr_device (in place of lr), grad_scale (NULL: 1)
  * and skip (nonzero: nothing is written and the step is not counted; NULL: never) are read on the device.  No two tensors
  * and no two calls in flight may share memory or `step` (a param that stands twice in the list is refused).
  */
+enum { ASD_ADAMW_UNBIASED = 256 };
 typedef struct {
   int64_t n;
   int32_t type, grad_type; /* asd_type */

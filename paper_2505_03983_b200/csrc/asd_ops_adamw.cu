@@ -3,7 +3,8 @@
 //   p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // Bound by memory: 28 bytes a parameter with moments and a master value in 32 bits and parameter and gradient in 16, 16 bytes with
-// moments in 8 bits.  117M parameters: 504 us in 32 bits (6.5 TB/s), 336 in 8 (5.6 TB/s; some 50 instructions an element beside
+// moments in 8 bits.  117M parameters: 504 us in 32 bits (6.5 TB/s), 336 in 8 (5.6 TB/s; 357 with random bits for its
+// codes; some 50 instructions an element beside
 // the memory's time; 508 us with integer conversions, types chosen at each operand and exact divisions).  A warp works on 256
 // neighbouring elements at a time, eight to a lane, which is also the block of elements that shares a scale in 8 bits, so that its
 // largest values are two warp-wide maxima.  The tensors' addresses are the launch's arguments (up to 32 KB of them): they need no
@@ -11,7 +12,15 @@
 //
 // 8 bits: m = M (q / 127) |q / 127| with M the block's largest |m|, sqrt(v) = R (q / 255)^2 with R its largest sqrt(v).  The square
 // puts the steps where the values are: half a step is 0.4 % of the largest value there, 4 % of one that is a hundredth of
-// it.  sqrt(v) is the denominator, so a v above 0 has a q of 1 at least.  What decays evenly is followed by the scales.
+// it.  sqrt(v) is the denominator, so a v above 0 has a q of 1 at least.
+//
+// Codes are rounded to the nearest, or (ASD_ADAMW_UNBIASED) up with the probability of their fraction.  Half a step of v is 2 / q of it, a
+// decay by beta2 = 0.999 only 0.001: rounded to the nearest, no code ever falls by decay while a large gradient lifts it, and sqrt(v)
+// in a block of gradients of one size, beside that in 32 bits, has a mean of 1.04 after 1000 steps, 1.14 after 3000 and 1.33 after 10000
+// (1.001, 1.002, 1.001 with the fraction's probability).  So it is with an m of less than 0.6 % of M at beta1 = 0.9, which then never
+// comes to 0.  Both are rounded so or neither: an m that stays beside a v that falls would be a step that grows.  As a code goes with
+// the root of m and the fourth root of v, roundings that leave its mean alone make v some 1.5 / q larger, which the mean of 1 / sqrt(v), the
+// step, gets back from v's spread.
 #include <math.h>
 
 #include <algorithm>
@@ -25,10 +34,11 @@ constexpr int kUnit = 256;     // elements of a warp at a time, and of a scale
 constexpr int kItem = 4;       // units that a warp takes in a row
 constexpr int kAdamBlock = 256;
 constexpr int kAdamSide = 3;  // blocks of an SM at a time
+constexpr int kUnbiased = 8 | ASD_ADAMW_UNBIASED;  // a kernel's BITS: 32, 8 or this
 // Blocks in all, for an SM.  In 32 bits memory is the time, and many blocks even out what the SMs get of it (117M parameters, 4: 604 us, 8:
 // 520, 16: 521, 48: 503); in 8 bits it is not all of it, and blocks beyond those that run together only begin again (3: 336 us, 6: 351, 32: 367).
 template <int BITS>
-constexpr int kAdamBlocks = BITS == 8 ? kAdamSide : 32;
+constexpr int kAdamBlocks = BITS == 32 ? 32 : kAdamSide;
 
 struct AdamTensor {
   void* param;
@@ -131,6 +141,46 @@ __device__ __forceinline__ uint32_t round_4(float a, float b, float c, float d) 
   const float2 up = make_float2(12582912.f, 12582912.f), x = add2(make_float2(a, b), up), y = add2(make_float2(c, d), up);
   return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040), __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
 }
+// What is added to codes before they are rounded to the nearest, 16 bits of r to a code: -0.5 to 0.5, both left out, so that a whole
+// number stays what it is.
+__device__ __forceinline__ float2 dither_pair(uint32_t r) {
+  constexpr float kIn = 1.f - 1.f / 32768.f;  // 128 + 16 bits, less 128.5, times this
+  return fma2(make_float2(__uint_as_float(__byte_perm(r, 0x43000000u, 0x7610)), __uint_as_float(__byte_perm(r, 0x43000000u, 0x7632))),
+              make_float2(kIn, kIn), make_float2(-128.5f * kIn, -128.5f * kIn));
+}
+// 64 random bits of eight neighbouring elements and a step by Philox-2x32 (7 rounds), and from them, by odd factors (digits of pi), 16 for
+// each of their codes of v (the first four words) and of m: each code's own bits are uniform over the steps, and the same in every run.
+__device__ __forceinline__ void dither_bits(int64_t at, int64_t step, uint32_t (&r)[8]) {
+  uint32_t a = (uint32_t)at, b = (uint32_t)step, key = (uint32_t)(at >> 32) ^ ((uint32_t)(step >> 32) << 16);
+#pragma unroll
+  for (int i = 0; i < 7; ++i) {
+    const uint32_t high = __umulhi(a, 0xd256d193u), low = a * 0xd256d193u;
+    a = high ^ key ^ b, b = low, key += 0x9e3779b9u;
+  }
+  r[0] = a, r[1] = b, r[2] = a * 0x243f6a89u, r[3] = b * 0x243f6a89u;
+  r[4] = b * 0x85a308d3u, r[5] = a * 0x85a308d3u, r[6] = b * 0x13198a2fu, r[7] = a * 0x13198a2fu;
+}
+// The dithers of a lane's eight elements.  They go by the element's place alone, not by how its lane came to it.
+template <bool WIDE>
+__device__ __forceinline__ void dithers(int64_t base, int lane, int64_t step, float2 (&m)[4], float2 (&v)[4]) {
+  uint32_t r[8];
+  if constexpr (WIDE) {
+    dither_bits(base / 8 + lane, step, r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = dither_pair(r[i]), m[i] = dither_pair(r[4 + i]);
+  } else {
+    const int word = (lane & 7) >> 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      dither_bits(element<false>(base, lane, i) / 8, step, r);
+      const uint32_t rv = word & 2 ? (word & 1 ? r[3] : r[2]) : (word & 1 ? r[1] : r[0]), rm = word & 2 ? (word & 1 ? r[7] : r[6]) : (word & 1 ? r[5] : r[4]);
+      const float2 pv = dither_pair(rv), pm = dither_pair(rm);
+      const float fv = lane & 1 ? pv.y : pv.x, fm = lane & 1 ? pm.y : pm.x;
+      i & 1 ? v[i >> 1].y = fv : v[i >> 1].x = fv;
+      i & 1 ? m[i >> 1].y = fm : m[i >> 1].x = fm;
+    }
+  }
+}
 // The moments that a block's codes stand for.
 __device__ __forceinline__ void moments_of(const uint32_t (&qm)[2], const uint32_t (&qv)[2], float2 scale, float (&fm)[8], float (&fv)[8]) {
   const float km = scale.x * (1.f / 16129.f), kv = scale.y * (1.f / 65025.f);
@@ -147,6 +197,7 @@ __device__ __forceinline__ void moments_of(const uint32_t (&qm)[2], const uint32
 
 struct Step {
   float b1, c1, b2, c2, eps, decay, size, root, scale;  // decay = lr wd, size = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
+  int64_t number;
 };
 // A unit of a tensor whose gradient has type G and whose values have type V.  The types are known where the unit is compiled: behind
 // a choice of type each operand's conversion would wait for it before the next one is asked for.
@@ -206,6 +257,17 @@ __device__ __forceinline__ void adam_unit(const AdamTensor& t, int64_t base, int
       // sqrt(v) is 0 or above 10^-23
       b[i] = fmaxf(sqrt_fast(y.x), __saturatef(r[i] * 1e30f)), b[i + 1] = fmaxf(sqrt_fast(y.y), __saturatef(r[i + 1] * 1e30f));
     }
+    if constexpr (BITS == kUnbiased) {
+      float2 dm[4], dv[4];
+      dithers<WIDE>(base, lane, s.number, dm, dv);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        // the block's largest are 127 and 255 but for the approximate root, and no dither may take them beyond
+        const float2 x = add2(make_float2(fminf(fmaxf(a[i], -127.f), 127.f), fminf(fmaxf(a[i + 1], -127.f), 127.f)), dm[i / 2]);
+        const float2 y = add2(make_float2(fminf(b[i], 255.f), fminf(b[i + 1], 255.f)), dv[i / 2]);
+        a[i] = x.x, a[i + 1] = x.y, b[i] = y.x, b[i + 1] = y.y;
+      }
+    }
     uint32_t qm[2], qv[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -264,6 +326,7 @@ __global__ void __launch_bounds__(kAdamBlock, kAdamSide) adamw_kernel(const __gr
   s.size = lr / -expm1f((float)steps * a.log_b1);
   s.root = 1.f / sqrtf(-expm1f((float)steps * a.log_b2));
   s.scale = a.grad_scale ? *a.grad_scale : 1.f;
+  s.number = steps;
   const int warps = gridDim.x * (kAdamBlock / 32);
   int low = 0;  // tensor of the item: they come in ascending order
   for (int64_t item = blockIdx.x * (kAdamBlock / 32) + (threadIdx.x >> 5); item < a.items; item += warps) {
@@ -367,7 +430,7 @@ void launch_bits(const asd_ops* o, const asd_adamw_args* q, cudaStream_t st) {
 }  // namespace
 
 void launch_adamw(const asd_ops* o, const asd_adamw_args* a, cudaStream_t st) {
-  a->bits == 32 ? launch_bits<32>(o, a, st) : launch_bits<8>(o, a, st);
+  a->bits == 32 ? launch_bits<32>(o, a, st) : a->bits == 8 ? launch_bits<8>(o, a, st) : launch_bits<kUnbiased>(o, a, st);
 }
 
 void launch_moments(const asd_ops* o, const asd_adamw_moments_args* q, cudaStream_t st) {

@@ -416,7 +416,7 @@ asd_status check_params(const asd_adamw_args* a) {
 }
 asd_status check_adamw(const asd_ops* o, const asd_adamw_args* a) {
   CHECK(check_handle(o, a));
-  REQUIRE(a->bits == 32 || a->bits == 8, ASD_ERR_INVALID_ARG, "bits must be 32 or 8: %d", a->bits);
+  REQUIRE(a->bits == 32 || a->bits == 8 || a->bits == (8 | ASD_ADAMW_UNBIASED), ASD_ERR_INVALID_ARG, "bits must be 32, 8 or 8 | ASD_ADAMW_UNBIASED: %d", a->bits);
   REQUIRE(a->count >= 0 && (a->count == 0 || a->tensors), ASD_ERR_INVALID_ARG, "%d tensors, and no list of them", a->count);
   REQUIRE(a->lr >= 0 && isfinite(a->lr) && a->eps >= 0 && isfinite(a->eps) && a->weight_decay >= 0 && isfinite(a->weight_decay), ASD_ERR_INVALID_ARG,
           "lr, eps and weight_decay must be finite and >= 0");
@@ -434,7 +434,7 @@ asd_status check_adamw(const asd_ops* o, const asd_adamw_args* a) {
     REQUIRE(all <= kAdamMost, ASD_ERR_UNSUPPORTED, "more than 2^36 elements in a call");
     REQUIRE(t.param && t.grad && t.m && t.v, ASD_ERR_INVALID_ARG, "tensor %d: param, grad, m and v must not be NULL", i);
     REQUIRE(!off_element(t.param, ops_type_size(t.type)) && !off_element(t.grad, ops_type_size(t.grad_type)) && !off_element(t.master, 4) &&
-                (a->bits == 8 || (!off_element(t.m, 4) && !off_element(t.v, 4))),
+                (a->bits != 32 || (!off_element(t.m, 4) && !off_element(t.v, 4))),
             ASD_ERR_INVALID_ARG, "tensor %d: an address is not a multiple of its element", i);
     REQUIRE(a->bits == 32 || (t.scales && !off_element(t.scales, 8)), ASD_ERR_INVALID_ARG, "tensor %d: scales must not be NULL, and on an 8-byte boundary", i);
   }

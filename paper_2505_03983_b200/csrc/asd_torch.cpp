@@ -533,7 +533,7 @@ struct TensorList {
 
 void adamw(int64_t ops, int device, const py::object& params_, const py::object& grads_, const py::object& m_, const py::object& v_, const Tensor& step, py::object lr,
            double beta1, double beta2, double eps, double weight_decay, const py::object& masters_, const py::object& scales_,
-           const OptTensor& grad_scale, const OptTensor& skip) {
+           const OptTensor& grad_scale, const OptTensor& skip, bool unbiased) {
   const Call c{(asd_ops*)ops, device};
   const TensorList params(params_, "params"), grads(grads_, "grads"), m(m_, "exp_avgs"), v(v_, "exp_avg_sqs"), masters(masters_, "masters"),
       scales(scales_, "scales");
@@ -544,6 +544,7 @@ void adamw(int64_t ops, int device, const py::object& params_, const py::object&
   std::vector<asd_adamw_tensor> list(n);
   std::vector<Tensor> held;  // gradients that had to be copied, until the call is enqueued
   const bool q8 = scales.given();
+  require(q8 || !unbiased, "adamw: unbiased is a rounding of moments in 8 bits, which have scales");
   for (size_t i = 0; i < n; ++i) {
     asd_adamw_tensor& t = list[i];
     const Tensor &p = params.at(i, "params"), &g = grads.at(i, "grads");
@@ -564,7 +565,7 @@ void adamw(int64_t ops, int device, const py::object& params_, const py::object&
     t.scales = q8 ? (float*)dense(c, scales.at(i, "scales"), "scales", (t.n + 255) / 256 * 2, at::kFloat) : nullptr;
   }
   asd_adamw_args a{};
-  a.count = (int32_t)n, a.bits = q8 ? 8 : 32, a.tensors = list.data();
+  a.count = (int32_t)n, a.bits = !q8 ? 32 : unbiased ? 8 | ASD_ADAMW_UNBIASED : 8, a.tensors = list.data();
   a.beta1 = beta1, a.beta2 = beta2, a.eps = eps, a.weight_decay = weight_decay;
   Tensor rate;
   if (THPVariable_Check(lr.ptr())) {

@@ -284,15 +284,17 @@ class AsdOps:
 
     # -- optimizer ---------------------------------------------------------------------------
     def adamw(self, params, grads, exp_avgs, exp_avg_sqs, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, masters=None, scales=None,
-              grad_scale=None, skip=None):
+              grad_scale=None, skip=None, unbiased=False):
         """A step of AdamW over lists of contiguous tensors, in place.  params and grads float32, float16 or bfloat16, each
         param once; masters, a list of float32 tensors with None for a param that has none (or None: for no param), hold the values
-        that params are rounded from.  Without scales exp_avgs and exp_avg_sqs are float32; with them they are int8 and uint8, and a tensor's scales float32 [(n + 255) // 256, 2] (include/asd_ops.h says
-        what they stand for; all start at zero).  step: int64 [2] on the device, zeros at first; its first word counts the steps.
-        lr: a number, or a float32 tensor of one element on the device.  grad_scale, a factor of the gradients, and skip, nonzero
-        for a step that is to be left out, are such tensors or None."""
+        that params are rounded from.  Without scales exp_avgs and exp_avg_sqs are float32; with them they are int8 and uint8,
+        and a tensor's scales float32 [(n + 255) // 256, 2] (include/asd_ops.h says what they stand for; all start at zero).
+        step: int64 [2] on the device, zeros at first; its first word counts the steps.  lr: a number, or a float32 tensor of one
+        element on the device.  grad_scale, a factor of the gradients, and skip, nonzero for a step that is to be left out, are
+        such tensors or None.  unbiased (with scales): codes are rounded up with the probability of their fraction, not to the
+        nearest, which over many steps does not follow a decay of less than half a step."""
         self._ext.adamw(self._handle, self.device, params, grads, exp_avgs, exp_avg_sqs, step, lr, betas[0], betas[1], eps, weight_decay, masters,
-                        scales, grad_scale, skip)
+                        scales, grad_scale, skip, unbiased)
 
     def adamw_moments(self, exp_avg, exp_avg_sq, scales, dtype=None):
         """(m, v) in `dtype` (float32) that the 8-bit moments of a tensor stand for."""

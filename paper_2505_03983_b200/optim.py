@@ -4,7 +4,8 @@
     opt = AdamW(net.parameters(), lr=1e-3, state_bits=8)      moments in 8 bits with two scales to 256 of them
 
 Parameters in float16 or bfloat16 get a float32 master value, which the step changes and rounds to the parameter: products read
-the 16-bit parameter as it is, with no cast of their own (masters=False: the parameter itself is changed, and rounded).
+the 16-bit parameter as it is, with no cast of their own (masters=False: the parameter itself is changed, and rounded).  Moments in
+8 bits are rounded up with the probability of their fraction, so that they follow decays of less than half of their steps.
 """
 from __future__ import annotations
 
@@ -81,7 +82,8 @@ class AdamW(torch.optim.Optimizer):
                     default_ops().adamw(params, [p.grad for p in params], [s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states],
                                         states[0]["step"], lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
                                         masters=[s.get("master") for s in states],
-                                        scales=[s["scales"] for s in states] if group["state_bits"] == 8 else None, grad_scale=grad_scale, skip=skip)
+                                        scales=[s["scales"] for s in states] if group["state_bits"] == 8 else None, grad_scale=grad_scale, skip=skip,
+                                        unbiased=group["state_bits"] == 8)
         return loss
 
     def load_state_dict(self, state_dict):
