@@ -219,7 +219,8 @@ asd_status asd_linear_forward_workspace(asd_ops* ops, const asd_linear_args* arg
 asd_status asd_linear_forward(asd_ops* ops, const asd_linear_args* args, void* cuda_stream);
 
 /*
- * Gradients:  dz = dy act'(z)  (rounded to the type for the products),
+ * Gradients:  dz = dy act'(z)  (rounded to the type for the products; F16 with a dy in F32: times a power of two that goes by dy's
+ * largest finite magnitude and is taken off their sums, so that a dz of 2^-28 of that still has all bits of F16),
  *   dx = dz w,   dw = dz^T x,   dbias = sum over rows of dz before that rounding  (bias_type);
  * the residual's is dy.  dy has dy_type: type, or F32.  x, w and `saved` as in the forward call (saved is not read for act
  * NONE); dx, dw, dbias may each be NULL (not computed).

@@ -308,6 +308,10 @@ asd_status run_linear_backward(const asd_ops* o, const asd_linear_backward_args*
   if (products && (acts || es == 4 || !mat_aligned(dy))) {
     dz = Mat{nullptr, rows, a->out, round_up(a->out, 8), 2};
     dz.p = r.dz = cut->take(rows * dz.ld * 2);
+    if (a->type == ASD_TYPE_F16 && es == 4) {  // what 32 bits hold may be far beyond the range of these 16
+      r.peaks = (uint32_t*)cut->take(4 * linear_peaks(o, rows, a->out));
+      r.unscale = (float*)cut->take(4);
+    }
   }
   if (a->dbias) r.part = (float*)cut->take(linear_part_bytes(o, rows, a->out));
   const int slices = a->dw ? sum_slices(o, a->out, a->width, rows, 2) : 1;  // dw is a sum over all rows: few outputs in slices
@@ -324,12 +328,12 @@ asd_status run_linear_backward(const asd_ops* o, const asd_linear_backward_args*
   if (a->dx) {  // dz w
     OpsGemm& g = list[n++] = OpsGemm{};
     g.epi = OPS_STORE, g.type = a->type, g.m = rows, g.n = a->width, g.k[0] = a->out, g.parts = 1;
-    g.a[0] = {dz, false}, g.b[0] = {w, true}, g.c[0] = a->dx, g.ldc = a->ld_dx;
+    g.a[0] = {dz, false}, g.b[0] = {w, true}, g.c[0] = a->dx, g.ldc = a->ld_dx, g.unscale = r.unscale;
   }
   if (a->dw) {  // dz^T x
     OpsGemm& g = list[n++] = OpsGemm{};
     g.epi = OPS_STORE, g.type = a->type, g.m = a->out, g.n = a->width, g.k[0] = rows, g.parts = 1;
-    g.a[0] = {dz, true}, g.b[0] = {x, true}, g.c[0] = a->dw, g.ldc = a->ld_dw;
+    g.a[0] = {dz, true}, g.b[0] = {x, true}, g.c[0] = a->dw, g.ldc = a->ld_dw, g.unscale = r.unscale;
     g.slices = slices, g.part = part;
   }
   return ops_gemm_list(o, list, n, st);

@@ -76,6 +76,7 @@ struct PairArgs {
   const float* scale_a;
   const float* scale_b;
   const float* bias;
+  const float* unscale;  // OPS_STORE: what the sums are multiplied by, or NULL
   int* err;
   // OPS_LINEAR
   int f16;        // the operands are F16, not BF16
@@ -541,6 +542,11 @@ op_pair_kernel(const __grid_constant__ PairMaps<products_of<EPI>> maps, const __
                 uint32_t r[32];
                 tc_ld32(t0 + c0 + 32 * h, r);
                 tc_wait_ld();
+                if (g.unscale) {
+                  const float by = *g.unscale;
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * by);
+                }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = pack16(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]), f16);
               } else {
@@ -683,6 +689,7 @@ struct JoinArgs {
     int m, n, slices, first;  // number of its first block
   } p[kMostProducts];
   int f16;
+  const float* unscale;  // or NULL
 };
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinArgs g) {
   __shared__ float tile[32][33];
@@ -700,6 +707,10 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinA
   for (int i = 0; i < p.slices; ++i) {
     const float4 v = from[i * slice];
     s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  if (g.unscale) {
+    const float by = *g.unscale;
+    s.x *= by, s.y *= by, s.z *= by, s.w *= by;
   }
   float* put = &tile[threadIdx.x & 31][4 * (threadIdx.x >> 5)];
   put[0] = s.x, put[1] = s.y, put[2] = s.z, put[3] = s.w;
@@ -805,6 +816,7 @@ asd_status launch_pair(const asd_ops* o, const OpsGemm* list, int count, cudaStr
   g.kept = q.kept;
   g.kept_cols = (int)((q.n + 31) / 32);
   g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias;
+  g.unscale = q.unscale;  // the list's products have the same one
   g.err = o->err;
   const int pairs = (int)std::min<int64_t>(units, o->num_sms / 2);
   ops_launch(op_pair_kernel<BN, EPI, ACT>, dim3(2 * pairs), dim3(kPairThreads), (size_t)C::kSmemBytes, st, 1, maps, g);
@@ -880,6 +892,7 @@ asd_status launch_join(const OpsGemm* list, int count, cudaStream_t st) {
   if (n == 0) return ASD_OK;
   for (int j = n; j < kMostProducts; ++j) g.p[j].first = INT_MAX;
   g.f16 = list[0].type == ASD_TYPE_F16;
+  g.unscale = list[0].unscale;
   ops_launch(join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, 1, g);
   return ops_launched("join of a sum's slices");
 }

@@ -96,6 +96,7 @@ struct OpsGemm {
   int64_t ldc;
   int slices;          // ops_gemm_list: > 1: the sum in that many slices, through `part` (part_bytes)
   float* part;
+  const float* unscale;  // OPS_STORE: a power of two on the device that the sums are multiplied by, or NULL
   uint8_t* kept;       // OPS_GATE: where the gate's two factors are kept, or NULL; OPS_GATE_GRAD: where they were; OPS_LINEAR: act'
   const float* scale_a;  // OPS_I8
   const float* scale_b;
@@ -158,7 +159,10 @@ struct LinearRows {
   int64_t ld_dz;
   void* dbias;          // or NULL
   float* part;          // linear_part_bytes
+  uint32_t* peaks;      // dz is written times a power of two that goes by dy's largest magnitude: linear_peaks words, or NULL (as it is)
+  float* unscale;       // with peaks: one over that power
 };
+int linear_peaks(const asd_ops* o, int64_t rows, int64_t out);
 int64_t linear_part_bytes(const asd_ops* o, int64_t rows, int64_t out);
 asd_status launch_linear_rows(const asd_ops* o, const LinearRows& a, cudaStream_t st);
 

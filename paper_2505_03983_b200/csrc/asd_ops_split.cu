@@ -44,6 +44,7 @@ struct SplitArgs {
   const float* scale_a;
   const float* scale_b;
   const float* bias;
+  const float* unscale;  // OPS_STORE: what the sums are multiplied by, or NULL
   int* err;
   // OPS_LINEAR
   int act, f16;  // f16: the operands are F16, not BF16
@@ -312,6 +313,11 @@ split_kernel(const __grid_constant__ SplitMaps maps, const __grid_constant__ Spl
           float y[4] = {__uint_as_float(v[i].x), __uint_as_float(v[i].y), __uint_as_float(v[i].z), __uint_as_float(v[i].w)};
           const int64_t at = row * g.ldc + col;
           if (EPI == OPS_STORE) {
+            if (g.unscale) {
+              const float by = *g.unscale;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[e] *= by;
+            }
             store4(g.c[0], at, y, cols, g.wide, f16);
           } else if (EPI == OPS_GATE) {
             float w[4] = {__uint_as_float(u[i].x), __uint_as_float(u[i].y), __uint_as_float(u[i].z), __uint_as_float(u[i].w)};
@@ -422,7 +428,7 @@ asd_status launch_split(const asd_ops* o, const OpsGemm& q, const SplitPlan& p, 
   g.wide_res = q.ldr % 4 == 0 && (uintptr_t)q.res % es4 == 0;
   g.c[0] = q.c[0], g.c[1] = q.c[1], g.ldc = q.ldc;
   g.kept = q.kept, g.kept_cols = (int)((q.n + 31) / 32);
-  g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias;
+  g.scale_a = q.scale_a, g.scale_b = q.scale_b, g.bias = q.bias, g.unscale = q.unscale;
   g.err = o->err;
   bool ok = true;  // only the maps that the kernel reads
   for (int i = 0; i < (EPI == OPS_GATE ? 2 : q.parts); ++i) ok = ok && encode_operand(&maps.w[i], q.b[i], q.type, I8, F);
