@@ -17,7 +17,9 @@ from .operators import default_ops
 class AdamW(torch.optim.Optimizer):
     """Parameters are contiguous CUDA tensors; one without a gradient is left as it is and its steps are not counted.  lr may be
     a float32 tensor of one element on the device, which a captured step then reads.  A step may be captured in a CUDA
-    graph once every parameter has its state, that is after a first step."""
+    graph once every parameter has its state, that is after a first step; the parameters that it steps together then do so for good: a
+    step in which some of them have no gradient is refused.  Parameters that take different steps are counted apart, with a launch for
+    each count."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, masters=True):
         if state_bits not in (8, 32):
@@ -27,7 +29,12 @@ class AdamW(torch.optim.Optimizer):
                 raise ValueError(f"{name} must be finite and >= 0: {v}")
         if not all(0 <= b < 1 for b in betas):
             raise ValueError(f"betas must be in [0, 1): {betas}")
+        self._captured = {}  # counters that a captured step moves on, by their identity
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay, state_bits=state_bits, masters=masters))
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        self._captured = {}
 
     def _new_state(self, p, group, fresh):
         if not p.is_cuda or not p.is_contiguous():
@@ -45,9 +52,10 @@ class AdamW(torch.optim.Optimizer):
             state["master"] = p.detach().float()
         self.state[p] = state
 
-    def _calls(self, group):
-        """The group's parameters that have a gradient, by the counter of their steps, which those share that have taken the same ones."""
-        fresh, ready, waiting = {}, {}, set()
+    def _plan(self, group):
+        """The group's parameters that have a gradient by the counter of their steps, which those share that have taken the same ones, those
+        without a state, and the counters that only some of those that share them move on this time.  Nothing is changed yet."""
+        ready, waiting, new = {}, set(), []
         for p in group["params"]:
             if p.grad is None:
                 if p in self.state:
@@ -55,16 +63,28 @@ class AdamW(torch.optim.Optimizer):
                 continue
             if p.grad.is_sparse:
                 raise RuntimeError("AdamW: sparse gradients are not supported")
-            if p not in self.state:
-                self._new_state(p, group, fresh)
+            if p in self.state:
+                ready.setdefault(id(self.state[p]["step"]), []).append(p)
+            else:
+                new.append(p)
+        split = [key for key in ready if key in waiting]
+        if split and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("AdamW: parameters that have stepped together so far no longer do: take such a step before one is captured")
+        if any(key in self._captured for key in split):  # its replays count the steps of all of them in one place
+            raise RuntimeError("AdamW: parameters whose steps were captured together cannot step apart; load_state_dict(state_dict()) parts the "
+                               "optimizer from the captured step, which then has to be captured again")
+        return ready, new, split
+
+    def _calls(self, group, ready, new, split):
+        """Lists of parameters that step together."""
+        for key in split:
+            step = self.state[ready[key][0]]["step"].clone()
+            for p in ready[key]:
+                self.state[p]["step"] = step
+        fresh = {}
+        for p in new:
+            self._new_state(p, group, fresh)
             ready.setdefault(id(self.state[p]["step"]), []).append(p)
-        for key, params in ready.items():
-            if key in waiting:  # some of those that share it stand still this time
-                if torch.cuda.is_current_stream_capturing():
-                    raise RuntimeError("AdamW: parameters that have stepped together so far no longer do: take such a step before one is captured")
-                step = self.state[params[0]]["step"].clone()
-                for p in params:
-                    self.state[p]["step"] = step
         return ready.values()
 
     @torch.no_grad()
@@ -75,10 +95,13 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        for group in self.param_groups:
-            for params in self._calls(group):
+        plans = [(group, self._plan(group)) for group in self.param_groups]
+        for group, plan in plans:
+            for params in self._calls(group, *plan):
                 states = [self.state[p] for p in params]
                 with torch.cuda.device(params[0].device):
+                    if torch.cuda.is_current_stream_capturing():
+                        self._captured[id(states[0]["step"])] = states[0]["step"]
                     default_ops().adamw(params, [p.grad for p in params], [s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states],
                                         states[0]["step"], lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
                                         masters=[s.get("master") for s in states],
@@ -90,6 +113,7 @@ class AdamW(torch.optim.Optimizer):
         """As torch's, but the states keep their types (torch's would give them the parameters'), and parameters that have taken the same
         number of steps share its counter again."""
         super().load_state_dict(state_dict)
+        self._captured = {}  # the states are other tensors now
         ids = [i for group in state_dict["param_groups"] for i in group["params"]]
         params = [p for group in self.param_groups for p in group["params"]]
         for i, p in zip(ids, params):
