@@ -4,8 +4,11 @@
     opt = AdamW(net.parameters(), lr=1e-3, state_bits=8)      moments in 8 bits with two scales to 256 of them
 
 Parameters in float16 or bfloat16 get a float32 master value, which the step changes and rounds to the parameter: products read
-the 16-bit parameter as it is, with no cast of their own (masters=False: the parameter itself is changed, and rounded).  Moments in
-8 bits are rounded up with the probability of their fraction, so that they follow decays of less than half of their steps.
+the 16-bit parameter as it is, with no cast of their own (masters=False: the parameter itself is changed, and rounded).  What else
+writes to a parameter is taken over into its master value: where the two no longer agree the next step begins from the
+parameter.  It sees that a parameter was written to by its version, which a write through .data or in a replayed graph does not
+change: refresh_masters() is for those.  Moments in 8 bits are rounded up with the probability of their fraction, so that they follow
+decays of less than half of their steps.
 """
 from __future__ import annotations
 
@@ -30,11 +33,12 @@ class AdamW(torch.optim.Optimizer):
         if not all(0 <= b < 1 for b in betas):
             raise ValueError(f"betas must be in [0, 1): {betas}")
         self._captured = {}  # counters that a captured step moves on, by their identity
+        self._versions = {}  # of parameters with a master value after their last step, by their identity
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay, state_bits=state_bits, masters=masters))
 
     def __setstate__(self, state):
         super().__setstate__(state)
-        self._captured = {}
+        self._captured, self._versions = {}, {}
 
     def _new_state(self, p, group, fresh):
         if not p.is_cuda or not p.is_contiguous():
@@ -50,6 +54,7 @@ class AdamW(torch.optim.Optimizer):
             state["scales"] = torch.zeros(((p.numel() + 255) // 256, 2), device=p.device)
         if group["masters"] and p.dtype != torch.float32:
             state["master"] = p.detach().float()
+            self._versions[id(p)] = None if p.is_inference() else p._version
         self.state[p] = state
 
     def _plan(self, group):
@@ -88,6 +93,17 @@ class AdamW(torch.optim.Optimizer):
         return ready.values()
 
     @torch.no_grad()
+    def _refresh(self, p, master):
+        """The elements of a master value that are not what its parameter was rounded from; the others keep their low bits."""
+        master.copy_(torch.where(p == master.to(p.dtype), master, p))
+
+    def refresh_masters(self):
+        """Takes over what parameters have been set to into their master values, however they were written."""
+        for p, state in self.state.items():
+            if "master" in state:
+                self._refresh(p, state["master"])
+
+    @torch.no_grad()
     def step(self, closure=None, grad_scale=None, skip=None):
         """grad_scale: a factor of the gradients; skip: nonzero for a step that is to be left out; float32 tensors of one element on
         the device, or None."""
@@ -99,21 +115,26 @@ class AdamW(torch.optim.Optimizer):
         for group, plan in plans:
             for params in self._calls(group, *plan):
                 states = [self.state[p] for p in params]
+                masters = [s.get("master") for s in states]
+                for p, master in zip(params, masters):
+                    if master is not None and not p.is_inference() and self._versions.get(id(p)) != p._version:
+                        self._refresh(p, master)
                 with torch.cuda.device(params[0].device):
                     if torch.cuda.is_current_stream_capturing():
                         self._captured[id(states[0]["step"])] = states[0]["step"]
                     default_ops().adamw(params, [p.grad for p in params], [s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states],
                                         states[0]["step"], lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
-                                        masters=[s.get("master") for s in states],
+                                        masters=masters,
                                         scales=[s["scales"] for s in states] if group["state_bits"] == 8 else None, grad_scale=grad_scale, skip=skip,
                                         unbiased=group["state_bits"] == 8)
+                self._versions.update((id(p), p._version) for p, master in zip(params, masters) if master is not None and not p.is_inference())
         return loss
 
     def load_state_dict(self, state_dict):
         """As torch's, but the states keep their types (torch's would give them the parameters'), and parameters that have taken the same
         number of steps share its counter again."""
         super().load_state_dict(state_dict)
-        self._captured = {}  # the states are other tensors now
+        self._captured, self._versions = {}, {}  # the states are other tensors now
         ids = [i for group in state_dict["param_groups"] for i in group["params"]]
         params = [p for group in self.param_groups for p in group["params"]]
         for i, p in zip(ids, params):

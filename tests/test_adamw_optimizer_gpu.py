@@ -99,3 +99,98 @@ def test_copies_of_an_optimizer_are_not_captured():
         for q in first[1:]:
             q.grad = None
         other.step()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_a_parameter_that_is_written_to(dtype):
+    """A step begins from what a 16-bit parameter has been set to, and from the master value where it is as the last step left it: against a
+    master value that is set beside the parameter."""
+    p, opt = make(dtype=dtype)
+    q, ref = make(dtype=dtype)
+    for _ in range(3):
+        opt.step(), ref.step()
+    new = rand((150,), 9, dtype)
+    nothing = opt.state[p[1]]["master"].clone()
+    with torch.no_grad():
+        p[0][100:250] = new
+        p[1].mul_(1.0)  # written to, and nothing changed: the master's low bits stay
+        q[0][100:250] = new
+    ref.state[q[0]]["master"][100:250] = new.float()
+    opt.step(), ref.step()
+    same(p, opt, q, ref)
+    assert not torch.equal(nothing, nothing.to(dtype).float())
+    assert float((p[0].detach()[100:250] - new).float().abs().max()) <= 2 * 1e-2 * 1.1 + 0.02 * float(new.abs().max())  # one step of lr away
+    # a whole network's values at once, as a checkpoint or an average is read in
+    net = torch.nn.ParameterList(p)
+    values = {k: rand(v.shape, 20, dtype) for k, v in net.state_dict().items()}
+    net.load_state_dict(values)
+    with torch.no_grad():
+        for a, v in zip(q, values.values()):
+            a.copy_(v)
+            ref.state[a]["master"].copy_(v)
+    opt.step(), ref.step()
+    same(p, opt, q, ref)
+    # through .data no version moves
+    for a in (p[0], q[0]):
+        a.data.copy_(new.repeat(2))
+    opt.refresh_masters()
+    ref.state[q[0]]["master"].copy_(new.repeat(2))
+    opt.step(), ref.step()
+    same(p, opt, q, ref)
+
+
+def test_a_parameter_that_is_not_a_number():
+    """Not a number in the parameter is taken over, and overwritten again."""
+    p, opt = make(dtype=torch.bfloat16)
+    opt.step()
+    with torch.no_grad():
+        p[0][3] = float("nan")
+    opt.step()
+    assert torch.isnan(opt.state[p[0]]["master"][3]) and int(torch.isnan(p[0]).sum()) == 1
+    with torch.no_grad():
+        p[0][3] = 1.0
+    opt.step()
+    assert torch.isfinite(p[0]).all() and abs(float(p[0][3]) - 1) < 0.1
+
+
+def test_values_and_state_are_loaded_in_either_order(tmp_path):
+    """The values of a network and the optimizer's state from a checkpoint, one before the other: the same steps; and with the
+    values alone steps that begin from them."""
+    p, opt = make(dtype=torch.bfloat16)
+    for _ in range(3):
+        opt.step()
+    torch.save([[v.detach() for v in p], opt.state_dict()], tmp_path / "state.pt")
+    opt.step()
+    for order in (0, 1):
+        q, other = make(dtype=torch.bfloat16)
+        other.step()
+        values, state = torch.load(tmp_path / "state.pt")
+        for what in (order, 1 - order):
+            if what:
+                other.load_state_dict(state)
+            else:
+                torch.nn.ParameterList(q).load_state_dict({str(i): v for i, v in enumerate(values)})
+        other.step()
+        same(p, opt, q, other)
+
+
+def test_a_captured_step_and_a_parameter_that_is_written_to():
+    """Replays change parameter and master together; what is written between them is taken over by an eager step."""
+    p, opt = make(dtype=torch.bfloat16)
+    q, ref = make(dtype=torch.bfloat16)
+    opt.step(), ref.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for _ in range(3):
+        graph.replay(), ref.step()
+    opt.step(), ref.step()
+    same(p, opt, q, ref)
+    with torch.no_grad():
+        for v in (p, q):
+            v[0].fill_(0.5)
+    opt.step(), ref.step()
+    graph.replay(), ref.step()
+    same(p, opt, q, ref)
+    for a in p:
+        assert torch.equal(a, opt.state[a]["master"].to(a.dtype))
