@@ -5,6 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <new>
 
 #include "asd_ops_internal.h"
@@ -397,25 +398,25 @@ asd_status check_block_backward(const asd_ops* o, const asd_block_rmsnorm_backwa
 }
 
 // ---- adamw ----------------------------------------------------------------------------------------------
-// Whether an address of a param stands in the list twice: its threads would then change it in an order of their own.
+// Whether an address of a param stands in the list twice: its threads would then change it in an order of their own.  No memory is asked
+// for: all that come after a batch of the list are looked up among it, in a table on the stack that is at most half full.
 asd_status check_params(const asd_adamw_args* a) {
-  size_t size = 64;
-  while (size < 2 * (size_t)a->count) size *= 2;
-  const void* few[512];
-  const void** slots = size <= 512 ? few : new (std::nothrow) const void*[size];
-  REQUIRE(slots, ASD_ERR_OOM, "out of host memory");
-  memset(slots, 0, size * sizeof(*slots));
-  int twice = -1;
-  for (int i = 0; i < a->count && twice < 0; ++i) {
-    if (a->tensors[i].n == 0) continue;
-    const void* p = a->tensors[i].param;
-    size_t at = (((uintptr_t)p >> 1) * 0x9e3779b97f4a7c15ull >> 32) & (size - 1);
-    while (slots[at] && slots[at] != p) at = (at + 1) & (size - 1);
-    if (slots[at]) twice = i;
-    slots[at] = p;
+  constexpr int kBatch = 2048;
+  const void* slots[2 * kBatch];
+  for (int from = 0; from < a->count; from += std::min(kBatch, a->count - from)) {
+    const int n = std::min(kBatch, a->count - from);
+    size_t size = 64;
+    while (size < 2 * (size_t)n) size *= 2;
+    memset(slots, 0, size * sizeof(*slots));
+    for (int i = from; i < a->count; ++i) {
+      if (a->tensors[i].n == 0) continue;
+      const void* p = a->tensors[i].param;
+      size_t at = (((uintptr_t)p >> 1) * 0x9e3779b97f4a7c15ull >> 32) & (size - 1);
+      while (slots[at] && slots[at] != p) at = (at + 1) & (size - 1);
+      REQUIRE(!slots[at], ASD_ERR_INVALID_ARG, "tensor %d: its param stands in the list twice", i);
+      if (i - from < n) slots[at] = p;
+    }
   }
-  if (slots != few) delete[] slots;
-  REQUIRE(twice < 0, ASD_ERR_INVALID_ARG, "tensor %d: its param stands in the list twice", twice);
   return ASD_OK;
 }
 asd_status check_adamw(const asd_ops* o, const asd_adamw_args* a) {
