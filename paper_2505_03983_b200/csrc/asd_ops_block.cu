@@ -240,17 +240,16 @@ __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 // 1 / sqrt(mean + eps), within 2 ulp.
 __device__ __forceinline__ float rho_fast(float sq, float inv_width, float eps) { return rsqrtf(fmaf(sq, inv_width, eps)); }
 
-// A block to a row.  TPR threads, kPer elements each (LONG: any number, read again for each pass).
-template <typename T, int VEC, int TPR, bool Q8, bool LONG>
-__global__ void __launch_bounds__(block_of<TPR>) block_norm_kernel(const BlockArgs a) {
-  constexpr int NV = kPer / VEC;
+// A block to a row.  kRowBlock threads, kPer elements each, in 16-byte pieces (LONG: any number, read again for each pass).
+constexpr int kRowBlock = 512;
+template <typename T, int VEC, bool Q8, bool LONG>
+__global__ void __launch_bounds__(kRowBlock) block_norm_kernel(const BlockArgs a) {
+  constexpr int TPR = kRowBlock, NV = kPer / VEC;
   __shared__ float buf_x[TPR / 32], buf_s[TPR / 32];
   __shared__ uint32_t buf_m[TPR / 32];
   dep_wait();
   dep_launch();
-  const int t = TPR == 32 ? (threadIdx.x & 31) : threadIdx.x;
-  const int row = TPR == 32 ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
-  if (row >= a.rows) return;  // whole warps: rows of a block do not share a barrier
+  const int t = threadIdx.x, row = blockIdx.x;
   const T* x = reinterpret_cast<const T*>(a.x) + row * a.ld_x;
   const T* r = reinterpret_cast<const T*>(a.r) + row * a.ld_r;
   T* so = reinterpret_cast<T*>(a.s) + row * a.ld_s;
@@ -586,8 +585,12 @@ __global__ void __launch_bounds__(kNarrowBlock) narrow_block_kernel(const BlockA
 }
 
 constexpr int kWalkSmem = 225 * 1024;
-// Shared memory that one of `side` blocks of an SM may ask for, next to what it declares and the 1 KB that a block costs.
-int walk_room(int side, int declared) { return std::min(kWalkSmem, 228 * 1024 / side - 1024 - declared); }
+// Shared memory that one of `side` blocks of an SM may ask for, next to what it declares and the 1 KB that a block costs; it is given out
+// in pieces of 128 bytes.
+int walk_room(int side, int declared) { return std::min(kWalkSmem, 228 * 1024 / side / 128 * 128 - 1024 - declared); }
+// What the kernels declare beside it: words a warp (forward: sums of x, two of s, a maximum; backward: two of eight sums), barriers, a flag.
+int walk_declared(int threads) { return threads / 32 * 16 + 128; }
+int grad_declared(int threads) { return threads / 32 * 64 + 128; }
 int walk_threads(int width) { return width <= 1024 ? 64 : width <= 2048 ? 128 : width <= 4096 ? 256 : width <= 8192 ? 512 : 1024; }
 // Bytes of a part of a row in the ring: all that the threads read, 32 more for one that does not start on 16 bytes.
 int walk_pitch(int width, int es, bool vec) { return walk_threads(width) * kWalkPer * es + (vec ? 0 : 32); }
@@ -599,7 +602,7 @@ void walk_rows_of(const asd_ops* o, BlockArgs n, cudaStream_t st) {
   const int stage_bytes = 2 * pitch + (n.ring_gate ? n.width * (n.g_f32 ? 4 : (int)sizeof(T)) : 0);  // one of them always finds room
   // as many blocks of an SM as its registers hold, unless shared memory then has no room for a row ahead
   int side = walk_side(threads);
-  auto room = [&]() { return walk_room(side, 512) / stage_bytes; };
+  auto room = [&]() { return walk_room(side, walk_declared(threads)) / stage_bytes; };
   while (side > 1 && room() < 2) --side;
   const int stages = std::max(1, std::min(VEC == 8 ? kMostStages : 2, room()));
   const dim3 grid(std::min(n.rows, side * o->num_sms)), block(threads);
@@ -622,12 +625,12 @@ void block_t(const asd_ops* o, const BlockArgs& n, bool vec, cudaStream_t st) {
     return;
   }
   if (n.width > kMostWalkWidth) {
-    ops_launch(vec ? block_norm_kernel<T, 8, 512, Q8, true> : block_norm_kernel<T, 1, 512, Q8, true>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    ops_launch(vec ? block_norm_kernel<T, 8, Q8, true> : block_norm_kernel<T, 1, Q8, true>, dim3(n.rows), dim3(kRowBlock), 0, st, 1, n);
     return;
   }
   // few rows: a block to each, with the row in registers
   if (vec && n.rows <= o->num_sms)
-    ops_launch(block_norm_kernel<T, 8, 512, Q8, false>, dim3(n.rows), dim3(512), 0, st, 1, n);
+    ops_launch(block_norm_kernel<T, 8, Q8, false>, dim3(n.rows), dim3(kRowBlock), 0, st, 1, n);
   else
     vec ? walk_rows_of<T, 8, Q8>(o, n, st) : walk_rows_of<T, 1, Q8>(o, n, st);
 }
@@ -1247,10 +1250,10 @@ GradPlan plan_grad(const asd_ops* o, int rows, int width, int es, bool vec, int 
     return p;
   }
   p.threads = walk_threads(width);
-  // the ranges have to be the same however the rows can be read, so that the workspace is: 16 bytes more for a staged part
+  // the ranges have to be the same however the rows can be read, so that the workspace is: 32 bytes more for a staged part
   const int most = 4 * walk_pitch(width, es, false);
   const int sums = p.threads * kWalkPer * 4;
-  auto room = [&](int side, int bytes) { return (walk_room(side, 2 * p.threads + 128) - sums) / bytes; };  // rows beside the sums
+  auto room = [&](int side, int bytes) { return (walk_room(side, grad_declared(p.threads)) - sums) / bytes; };  // rows beside the sums
   int side = grad_side(p.threads);
   while (side > 1 && room(side, most) < 2) side /= 2;
   p.ranges = p.blocks = std::min(rows, side * o->num_sms);
