@@ -307,7 +307,7 @@ asd_status asd_block_rmsnorm_backward(asd_ops* ops, const asd_block_rmsnorm_back
  * A step of AdamW over `count` tensors (any number of them, of any size):
  *   g = grad grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32, with t the number of steps after this one.  p is the master value where there is one, which is then rounded to
+ * in fp32 (an eps between 0 and 2^-126 is 2^-126), with t the number of steps after this one.  p is the master value where there is one, which is then rounded to
  * the parameter; otherwise the parameter itself, rounded to its type.
  * bits 32: m and v are fp32.  bits 8: m int8 and v uint8 with two scales (M, R) to each 256 neighbouring elements of a
  * tensor, all zero at first:

@@ -21,6 +21,7 @@
 // comes to 0.  Both are rounded so or neither: an m that stays beside a v that falls would be a step that grows.  As a code goes with
 // the root of m and the fourth root of v, roundings that leave its mean alone make v some 1.5 / q larger, which the mean of 1 / sqrt(v), the
 // step, gets back from v's spread.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -404,7 +405,8 @@ void launch_list(const asd_ops* o, const asd_adamw_args* q, const asd_adamw_tens
   }
   a.items = (int)items, a.advance = last;
   a.b1 = (float)q->beta1, a.c1 = (float)(1 - q->beta1), a.b2 = (float)q->beta2, a.c2 = (float)(1 - q->beta2);
-  a.eps = (float)q->eps, a.wd = (float)q->weight_decay, a.lr = (float)q->lr;
+  // the kernel's reciprocal takes what is below the least normal number for 0, and 0 / 0 is not what a gradient of 0 is to give
+  a.eps = q->eps > 0 ? std::max((float)q->eps, FLT_MIN) : 0.f, a.wd = (float)q->weight_decay, a.lr = (float)q->lr;
   a.log_b1 = (float)log(q->beta1), a.log_b2 = (float)log(q->beta2);
   a.lr_at = q->lr_device, a.grad_scale = q->grad_scale, a.skip = q->skip, a.step = q->step;
   const int64_t blocks = (items + kAdamBlock / 32 - 1) / (kAdamBlock / 32), most = kAdamBlocks<BITS> * (int64_t)o->num_sms;
