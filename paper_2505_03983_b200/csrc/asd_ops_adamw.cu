@@ -3,12 +3,11 @@
 //   p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // Bound by memory: 28 bytes a parameter with moments and a master value in 32 bits and parameter and gradient in 16, 16 bytes with
-// moments in 8 bits.  117M parameters: 504 us in 32 bits (6.5 TB/s), 336 in 8 (5.6 TB/s; 357 with random bits for its
-// codes; some 50 instructions an element beside
-// the memory's time; 508 us with integer conversions, types chosen at each operand and exact divisions).  A warp works on 256
-// neighbouring elements at a time, eight to a lane, which is also the block of elements that shares a scale in 8 bits, so that its
-// largest values are two warp-wide maxima.  The tensors' addresses are the launch's arguments (up to 32 KB of them): they need no
-// copy of their own and a captured graph keeps them.
+// moments in 8 bits.  117M parameters: 504 us in 32 bits (6.5 TB/s), 336 in 8 (5.6 TB/s; some 50 instructions an element beside
+// the memory's time; 508 us with integer conversions, types chosen at each operand and exact divisions), 357 with random bits for
+// the codes (5.3 TB/s, 54 % of the issue slots where it was 44).  A warp works on 256 neighbouring elements at a time, eight to a lane,
+// which is also the block of elements that shares a scale in 8 bits, so that its largest values are two warp-wide maxima.  The tensors'
+// addresses are the launch's arguments (up to 32 KB of them): they need no copy of their own and a captured graph keeps them.
 //
 // 8 bits: m = M (q / 127) |q / 127| with M the block's largest |m|, sqrt(v) = R (q / 255)^2 with R its largest sqrt(v).  The square
 // puts the steps where the values are: half a step is 0.4 % of the largest value there, 4 % of one that is a hundredth of
